@@ -200,10 +200,8 @@ def prepare(case, seed):
         elif path == "paged":
             size = cq.cq_paged_attn_workspace_bytes(n, st["offsets"][-1], case["n_new"], hq, hkv, D, case["c"], case["b"],
                                                     case["page"], st["page_table"].shape[1], case["window"], case["sinks"])
-        elif path == "mass":
-            size = cq.cq_attn_mass_workspace_bytes(n, case["n_new"], hq, hkv, D, case["c"], case["b"], case["capacity"])
         else:
-            size = cq.cq_evict_workspace_bytes(n, hkv, D, case["c"], case["b"], case["capacity"], case["keep"])
+            size = cq.cq_attn_mass_workspace_bytes(n, max(1, case.get("n_new", 0)), hq, hkv, D, case["c"], case["b"], case["capacity"])
         st["workspace"] = torch.empty(max(size, 256), dtype=torch.uint8, device=DEV)
     return st
 
@@ -231,7 +229,7 @@ def _run_own(st):
         return cq.cq_attn_mass(st["q"], st["k_codes"], st["k_cb"], st["seq_lens"], st["scale"], c, b, cap, st["mass"],
                                mass_out=st["mass_out"], workspace=st["workspace"])
     kept, lens = cq.cq_evict(st["mass"], st["k_codes"], st["v_codes"], st["seq_lens"], k["head_dim"], c, b, cap, k["keep"], k["sinks"], k["recent"],
-                             st["k_out"], st["v_out"], st["mass_out"], st["room"], workspace=st["workspace"])
+                             st["k_out"], st["v_out"], st["mass_out"], st["room"])
     return dict(kept=kept, lens=lens, k=st["k_out"], v=st["v_out"], mass=st["mass_out"])
 
 

@@ -16,7 +16,10 @@
  * cq_prefill_attn (causal attention of a run of new tokens over the coded cache),
  * cq_decode_attn_static (no caller workspace), cq_decode_step_host (one decode
  * step from host buffers) and the centroid learning of Section 3.2.1
- * (cq_kmeanspp_init, cq_lloyd_step, cq_learn_centroids).
+ * (cq_kmeanspp_init, cq_lloyd_step, cq_learn_centroids); and, for caches of bounded memory,
+ * cq_window_attn (sliding window and first tokens), cq_paged_append and cq_paged_attn (codes in
+ * pages, ragged chunks of new tokens), cq_attn_mass and cq_evict (accumulated attention weight
+ * of cached tokens, and eviction by it).
  *
  * General rules
  *   - Every pointer is a DEVICE pointer unless its name ends in _host.  The
@@ -423,6 +426,130 @@ int cq_decode_step_host(const void *q_host, const void *k_new_host, const void *
                         int n_seq, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
                         int64_t max_tokens, float *out_host, void *workspace, size_t workspace_bytes,
                         void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Coded caches of bounded memory: attention with a sliding window, attention over pages, and eviction by accumulated
+ * attention weight.  (The paper has no counterpart; Eq. 1 and Section 3.2 give what is attended: the CQ reconstructions.)
+ *
+ * Common to these calls: queries, codebooks and outputs are fp16 (Section 4.3 of the paper stores the centroids in fp16;
+ * encode with the same centroids widened to fp32), positions are below 2^30, scores, softmax sums and masses are held in
+ * fp32.  A workspace's contents on entry are ignored; two calls that overlap on the GPU need one each.  Lengths outside of
+ * [0, capacity] are clamped.
+ *
+ * Visible tokens.  The query tokens of a sequence are its newest cached tokens (their codes are in the cache already and
+ * seq_lens counts them): query i of n sits at position seq_lens[s] - n + i.  A query at position p sees cached token t where
+ *     t <= p   and   (window == 0  or  t < n_sinks  or  t > p - window),
+ * so window counts the query's own token, and the n_sinks first tokens stay visible behind the window.  A query that sees
+ * nothing (its position is negative, or no page is named for what it sees) gets a zero row.
+ *
+ * Kernels.  head_dim 128 with one byte per code, c = 2, 4 or 8: sequences with up to 16 (query token, query head of a KV head)
+ * rows go through a kernel whose warps gather centroids from shared memory straight into tensor-core fragments, sequences
+ * with more rows through one on tcgen05 (every wait in it is bounded; should one give up, its rows are NaN).  Softmax weights
+ * are rounded to fp16 for the second product, sums are fp32.  Every other supported shape runs on plain kernels.
+ * _variant picks: 0 = automatic, 1 = plain kernel, 2 = the gather kernel, 3 = the tcgen05 kernel (CQ_ERR_UNSUPPORTED where
+ * the shape has none).
+ */
+
+/*
+ * Attention of the n_q_tokens newest tokens of every sequence over a contiguous cache (cq_decode_attn's layout), with a
+ * sliding window and sinks.  n_q_tokens = 1 is a decode step's attention.
+ *
+ *   q_fp16, out_fp16   fp16 [n_seq][n_q_tokens][n_q_heads][head_dim], 16-byte aligned
+ *   k_cb_fp16, v_cb_fp16   fp16 [n_kv_heads][G][2^b][c], 16-byte aligned
+ *   window   0: all tokens up to the query's
+ *   workspace   at least cq_window_attn_workspace_bytes(...) bytes, 16-byte aligned
+ * CQ_ERR_SHAPE for n_q_tokens < 1 or > max_tokens, a negative window or n_sinks.
+ */
+size_t cq_window_attn_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
+                                      int64_t max_tokens, int64_t window, int64_t n_sinks);
+int cq_window_attn(const void *q_fp16, const void *k_codes, const void *v_codes, const void *k_cb_fp16, const void *v_cb_fp16,
+                   const int32_t *seq_lens, float scale, int64_t window, int64_t n_sinks, int n_seq, int n_q_tokens,
+                   int n_q_heads, int n_kv_heads, int head_dim, int c, int b, int64_t max_tokens, void *out_fp16,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int cq_window_attn_variant(const void *q_fp16, const void *k_codes, const void *v_codes, const void *k_cb_fp16,
+                   const void *v_cb_fp16, const int32_t *seq_lens, float scale, int64_t window, int64_t n_sinks, int n_seq,
+                   int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b, int64_t max_tokens,
+                   void *out_fp16, void *workspace, size_t workspace_bytes, int variant, void *stream);
+
+/*
+ * Attention of ragged chunks of new tokens over a paged cache.  A page holds page_tokens (a multiple of 16) tokens of all
+ * KV heads: a pool of n_pages pages is a code buffer of cq_codes_bytes(n_pages, page_tokens, ...) bytes whose "sequences"
+ * are the pages.  Token t of sequence s lies in page page_table[s][t / page_tokens].
+ *
+ *   q_fp16, out_fp16   fp16 [n_rows][n_q_heads][head_dim]: the new tokens of all sequences, back to back
+ *   q_offsets    [n_seq + 1] int32, device, ascending: the rows of sequence s are q_offsets[s] ... q_offsets[s + 1] - 1
+ *                (none, one or many).  Rows of no sequence are left as they were in out.  Offsets are clamped to n_rows.
+ *   max_q        no sequence has more new tokens (counts above are taken as max_q)
+ *   page_table   [n_seq][pages_per_seq] int32, device; entries that hold no attended token are not used, the tokens of an
+ *                entry outside of [0, n_pages) count as absent
+ *   seq_lens     [n_seq] int32, device: cached tokens, the new ones included
+ *   window, n_sinks   as above; window 0: all tokens
+ */
+size_t cq_paged_attn_workspace_bytes(int n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_kv_heads, int head_dim, int c,
+                                     int b, int64_t page_tokens, int64_t pages_per_seq, int64_t window, int64_t n_sinks);
+int cq_paged_attn(const void *q_fp16, const int32_t *q_offsets, const void *k_pages, const void *v_pages,
+                  const void *k_cb_fp16, const void *v_cb_fp16, const int32_t *page_table, const int32_t *seq_lens,
+                  float scale, int64_t window, int64_t n_sinks, int n_seq, int64_t n_rows, int max_q, int n_q_heads,
+                  int n_kv_heads, int head_dim, int c, int b, int64_t n_pages, int64_t page_tokens, int64_t pages_per_seq,
+                  void *out_fp16, void *workspace, size_t workspace_bytes, void *stream);
+int cq_paged_attn_variant(const void *q_fp16, const int32_t *q_offsets, const void *k_pages, const void *v_pages,
+                  const void *k_cb_fp16, const void *v_cb_fp16, const int32_t *page_table, const int32_t *seq_lens,
+                  float scale, int64_t window, int64_t n_sinks, int n_seq, int64_t n_rows, int max_q, int n_q_heads,
+                  int n_kv_heads, int head_dim, int c, int b, int64_t n_pages, int64_t page_tokens, int64_t pages_per_seq,
+                  void *out_fp16, void *workspace, size_t workspace_bytes, int variant, void *stream);
+
+/*
+ * The way into the pages: the codes of the new tokens (cq_encode_kv's, with its fp32 codebooks) are written at the positions
+ * seq_lens[s] - n ... seq_lens[s] - 1 of their sequences (q_offsets, page_table, seq_lens as in cq_paged_attn: the same
+ * arrays serve both calls).  Positions outside of the capacity, and pages outside of the pool, are skipped; other positions
+ * are untouched.  Two sequences must not have new tokens in the same page.
+ *   k_fp16, v_fp16   fp16 [n_rows][n_heads][head_dim], 16-byte aligned;  k_pages, v_pages: two buffers
+ */
+size_t cq_paged_append_workspace_bytes(int64_t n_rows, int n_heads, int head_dim, int c, int b);
+int cq_paged_append(const void *k_fp16, const void *v_fp16, const int32_t *q_offsets, const float *k_cb, const float *v_cb,
+                    const int32_t *page_table, const int32_t *seq_lens, int n_seq, int64_t n_rows, int max_q, int n_heads,
+                    int head_dim, int c, int b, int64_t n_pages, int64_t page_tokens, int64_t pages_per_seq, void *k_pages,
+                    void *v_pages, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight that every cached token receives from the n_q_tokens newest tokens (causal, no window), summed over
+ * them and over the query heads of a KV head, on top of what it has received so far:
+ *   mass_out[s][h][t] = mass_in[s][h][t] + sum over queries i and query heads r of h of softmax_t(scale <q_ir, Khat_t>)
+ *
+ *   mass_in      NULL (zeros), or fp32 [n_seq][n_kv_heads][max_tokens], device
+ *   mass_out     the same shape, may be mass_in; positions from seq_lens[s] on are left as they were
+ *   workspace    at least cq_attn_mass_workspace_bytes(...) bytes, 16-byte aligned
+ * Sums are formed in a fixed order: two calls on the same inputs give the same bits.
+ * variant: 0 = automatic, 1 = plain kernels, 2 = tensor-core kernel (head_dim 128, one byte per code, c = 2, 4 or 8).
+ */
+size_t cq_attn_mass_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
+                                    int64_t max_tokens);
+int cq_attn_mass(const void *q_fp16, const void *k_codes, const void *k_cb_fp16, const int32_t *seq_lens, float scale,
+                 const float *mass_in, int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
+                 int64_t max_tokens, float *mass_out, void *workspace, size_t workspace_bytes, void *stream);
+int cq_attn_mass_variant(const void *q_fp16, const void *k_codes, const void *k_cb_fp16, const int32_t *seq_lens, float scale,
+                 const float *mass_in, int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
+                 int64_t max_tokens, float *mass_out, void *workspace, size_t workspace_bytes, int variant, void *stream);
+
+/*
+ * Eviction by mass.  Of the n = min(seq_lens[s], max_tokens) tokens of every (sequence, head) stay the n_sinks first, the
+ * n_recent last and, of the others, those of largest mass (of equal masses the lower position; a NaN counts as larger than
+ * every number), n_keep in all, or all n where n <= n_keep.  Their codes and masses move, in their old order, to the
+ * positions 0, 1, ... of the output cache, which may be the input cache.
+ *
+ *   k_codes, v_codes, mass   a cache of capacity max_tokens and its masses, as in cq_attn_mass
+ *   k_codes_out, v_codes_out, mass_out   a cache of capacity out_max_tokens >= n_keep; either all three are the inputs
+ *                themselves (with out_max_tokens == max_tokens), or none overlaps an input.  The rest of the last 16-token
+ *                block of codes is zeroed, everything behind it is left as it was.
+ *   kept_out     int32 [n_seq][n_heads][n_keep]: the old position of every token that stays, ascending, -1 behind the last
+ *   seq_lens_out [n_seq] int32, not seq_lens: min(n, n_keep)
+ * Needs no workspace.  CQ_ERR_SHAPE for n_keep < 1 or > out_max_tokens, n_sinks + n_recent > n_keep, or buffers that alias
+ * otherwise.
+ */
+int cq_evict(const float *mass, const void *k_codes, const void *v_codes, const int32_t *seq_lens, int n_seq, int n_heads,
+             int head_dim, int c, int b, int64_t max_tokens, int64_t n_keep, int64_t n_sinks, int64_t n_recent,
+             int64_t out_max_tokens, float *mass_out, void *k_codes_out, void *v_codes_out, int32_t *kept_out,
+             int32_t *seq_lens_out, void *stream);
 
 #ifdef __cplusplus
 }

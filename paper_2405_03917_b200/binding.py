@@ -23,7 +23,10 @@ _LIB_PATH = os.path.join(_HERE, "libcq.so")
 EXPORTS = ["cq_layout_version", "cq_status_string", "cq_codes_bytes", "cq_encode", "cq_encode_variant", "cq_encode_kv",
            "cq_codes_to_rowmajor", "cq_codes_from_rowmajor", "cq_decode_attn_workspace_bytes", "cq_decode_attn",
            "cq_decode_attn_variant", "cq_decode_attn_rope", "cq_decode_attn_rope_variant", "cq_prefill_attn", "cq_prefill_attn_variant", "cq_decode_attn_static", "cq_decode_step_workspace_bytes", "cq_decode_step_launches", "cq_decode_step", "cq_decode_step_host_workspace_bytes",
-           "cq_decode_step_host", "cq_learn_workspace_bytes", "cq_kmeanspp_init", "cq_lloyd_step", "cq_learn_centroids"]
+           "cq_decode_step_host", "cq_learn_workspace_bytes", "cq_kmeanspp_init", "cq_lloyd_step", "cq_learn_centroids",
+           "cq_window_attn_workspace_bytes", "cq_window_attn", "cq_window_attn_variant", "cq_paged_attn_workspace_bytes", "cq_paged_attn",
+           "cq_paged_attn_variant", "cq_paged_append_workspace_bytes", "cq_paged_append", "cq_attn_mass_workspace_bytes", "cq_attn_mass",
+           "cq_attn_mass_variant", "cq_evict"]
 
 
 class CQError(RuntimeError):
@@ -100,6 +103,25 @@ def lib() -> ctypes.CDLL:
         L.cq_decode_step_host.restype = i32
         L.cq_decode_step_host.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, f32, i32, i32, i32, i32, i32, i32, i64,
                                           vp, vp, sz, vp]
+        L.cq_window_attn_workspace_bytes.restype = sz
+        L.cq_window_attn_workspace_bytes.argtypes = [i32] * 7 + [i64] * 3
+        window = [vp] * 6 + [f32, i64, i64] + [i32] * 7 + [i64, vp, vp, sz]
+        L.cq_paged_attn_workspace_bytes.restype = sz
+        L.cq_paged_attn_workspace_bytes.argtypes = [i32, i64] + [i32] * 6 + [i64] * 4
+        paged = [vp] * 8 + [f32, i64, i64, i32, i64] + [i32] * 6 + [i64] * 3 + [vp, vp, sz]
+        L.cq_attn_mass_workspace_bytes.restype = sz
+        L.cq_attn_mass_workspace_bytes.argtypes = [i32] * 7 + [i64]
+        mass = [vp] * 4 + [f32, vp] + [i32] * 7 + [i64, vp, vp, sz]
+        for name, args in (("cq_window_attn", window), ("cq_paged_attn", paged), ("cq_attn_mass", mass)):
+            for f, more in ((getattr(L, name), []), (getattr(L, name + "_variant"), [i32])):
+                f.restype = i32
+                f.argtypes = args + more + [vp]
+        L.cq_paged_append_workspace_bytes.restype = sz
+        L.cq_paged_append_workspace_bytes.argtypes = [i64] + [i32] * 4
+        L.cq_paged_append.restype = i32
+        L.cq_paged_append.argtypes = [vp] * 7 + [i32, i64] + [i32] * 5 + [i64] * 3 + [vp, vp, vp, sz, vp]
+        L.cq_evict.restype = i32
+        L.cq_evict.argtypes = [vp] * 4 + [i32] * 5 + [i64] * 5 + [vp] * 6
         _lib = L
     return _lib
 
@@ -495,3 +517,197 @@ def cq_learn_centroids(x: torch.Tensor, weights: Optional[torch.Tensor], uniform
                                   ws.numel(), _stream())
     _check(st, "cq_learn_centroids")
     return out, obj
+
+
+# ------------------------------------------------------------------------------ caches of bounded memory
+# These calls run on the device of their tensors and on its current stream, whatever device is current.
+
+def _one_device(*tensors):
+    dev = tensors[0].device
+    for t in tensors[1:]:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    return torch.cuda.device(dev)
+
+
+def _book16(t: torch.Tensor, n_heads: int, head_dim: int, c: int, b: int, name: str) -> int:
+    if tuple(t.shape) != (n_heads, head_dim // max(c, 1), 1 << b, c):
+        raise ValueError(f"{name} shape {tuple(t.shape)} does not match heads/groups/centroids")
+    return _dev(t, torch.float16, name)
+
+
+def _hold(need: int, **buffers) -> None:
+    for name, t in buffers.items():
+        if need and t.numel() < need:
+            raise ValueError(f"{name} holds {t.numel()} elements, {need} needed")
+
+
+def _length(t: torch.Tensor, n: int, name: str) -> int:
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return _dev(t, torch.int32, name)
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    return given if given is not None else torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+
+
+def _like(out: Optional[torch.Tensor], shape, dtype, device, name: str) -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} shape {tuple(out.shape)}, expected {tuple(shape)}")
+    _dev(out, dtype, name)
+    return out
+
+
+def cq_window_attn_workspace_bytes(n_seq: int, n_q_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, c: int, b: int,
+                                   max_tokens: int, window: int, n_sinks: int = 0) -> int:
+    return int(lib().cq_window_attn_workspace_bytes(n_seq, n_q_tokens, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens, window, n_sinks))
+
+
+def cq_window_attn(q: torch.Tensor, k_codes: torch.Tensor, v_codes: torch.Tensor, k_cb: torch.Tensor, v_cb: torch.Tensor,
+                   seq_lens: torch.Tensor, scale: float, c: int, b: int, max_tokens: int, window: int, n_sinks: int = 0,
+                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, variant: int = 0) -> torch.Tensor:
+    """Attention of the n_q newest cached tokens with a sliding window (0: none) and the n_sinks first tokens visible.
+    q fp16 (n_seq, n_q, Hq, head_dim); codebooks fp16 (Hkv, G, 2^b, c); seq_lens int32 (n_seq,) counts the new tokens.
+    Returns out fp16 like q."""
+    n_seq, n_q, n_q_heads, head_dim = q.shape
+    n_kv_heads = k_cb.shape[0]
+    _hold(cq_codes_bytes(n_seq, max_tokens, n_kv_heads, head_dim, c, b), k_codes=k_codes, v_codes=v_codes)
+    with _one_device(q, k_codes, v_codes, k_cb, v_cb, seq_lens, out, workspace):
+        out = _like(out, q.shape, torch.float16, q.device, "out")
+        workspace = _workspace(workspace, cq_window_attn_workspace_bytes(n_seq, n_q, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens, window, n_sinks), q.device)
+        st = lib().cq_window_attn_variant(_dev(q, torch.float16, "q"), _dev(k_codes, torch.uint8, "k_codes"), _dev(v_codes, torch.uint8, "v_codes"),
+                                          _book16(k_cb, n_kv_heads, head_dim, c, b, "k_cb"), _book16(v_cb, n_kv_heads, head_dim, c, b, "v_cb"),
+                                          _length(seq_lens, n_seq, "seq_lens"), float(scale), window, n_sinks, n_seq, n_q, n_q_heads, n_kv_heads,
+                                          head_dim, c, b, max_tokens, out.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                          variant, _stream())
+    _check(st, "cq_window_attn")
+    return out
+
+
+def cq_paged_attn_workspace_bytes(n_seq: int, n_rows: int, max_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int, c: int, b: int,
+                                  page_tokens: int, pages_per_seq: int, window: int = 0, n_sinks: int = 0) -> int:
+    return int(lib().cq_paged_attn_workspace_bytes(n_seq, n_rows, max_q, n_q_heads, n_kv_heads, head_dim, c, b, page_tokens, pages_per_seq,
+                                                   window, n_sinks))
+
+
+def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, page_tokens: int, n_heads: int, head_dim: int, c: int, b: int) -> int:
+    """Whole pages that both buffers hold."""
+    page = cq_codes_bytes(16, page_tokens, n_heads, head_dim, c, b) // 16
+    return min(k_pages.numel(), v_pages.numel()) // page if page else 1
+
+
+def cq_paged_attn(q: torch.Tensor, q_offsets: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_cb: torch.Tensor,
+                  v_cb: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, scale: float, c: int, b: int, page_tokens: int,
+                  max_q: int, window: int = 0, n_sinks: int = 0, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, variant: int = 0) -> torch.Tensor:
+    """Attention of ragged chunks of new tokens over a paged cache.  q fp16 (n_rows, Hq, head_dim), rows q_offsets[s] ... of
+    sequence s (int32, n_seq + 1 entries, at most max_q per sequence); k_pages / v_pages uint8 pools of pages of page_tokens tokens;
+    page_table int32 (n_seq, pages_per_seq); seq_lens counts the new tokens.  Returns out fp16 like q; rows of no sequence are left
+    as they were."""
+    n_rows, n_q_heads, head_dim = q.shape
+    n_kv_heads = k_cb.shape[0]
+    n_seq, pages_per_seq = page_table.shape
+    n_pages = _pages(k_pages, v_pages, page_tokens, n_kv_heads, head_dim, c, b)
+    with _one_device(q, q_offsets, k_pages, v_pages, k_cb, v_cb, page_table, seq_lens, out, workspace):
+        out = _like(out, q.shape, torch.float16, q.device, "out")
+        workspace = _workspace(workspace, cq_paged_attn_workspace_bytes(n_seq, n_rows, max_q, n_q_heads, n_kv_heads, head_dim, c, b, page_tokens,
+                                                                        pages_per_seq, window, n_sinks), q.device)
+        if n_rows == 0:
+            return out
+        st = lib().cq_paged_attn_variant(_dev(q, torch.float16, "q"), _length(q_offsets, n_seq + 1, "q_offsets"), _dev(k_pages, torch.uint8, "k_pages"),
+                                         _dev(v_pages, torch.uint8, "v_pages"), _book16(k_cb, n_kv_heads, head_dim, c, b, "k_cb"),
+                                         _book16(v_cb, n_kv_heads, head_dim, c, b, "v_cb"), _dev(page_table, torch.int32, "page_table"),
+                                         _length(seq_lens, n_seq, "seq_lens"), float(scale), window, n_sinks, n_seq, n_rows, max_q, n_q_heads,
+                                         n_kv_heads, head_dim, c, b, n_pages, page_tokens, pages_per_seq, out.data_ptr(),
+                                         _dev(workspace, torch.uint8, "workspace"), workspace.numel(), variant, _stream())
+    _check(st, "cq_paged_attn")
+    return out
+
+
+def cq_paged_append_workspace_bytes(n_rows: int, n_heads: int, head_dim: int, c: int, b: int) -> int:
+    return int(lib().cq_paged_append_workspace_bytes(n_rows, n_heads, head_dim, c, b))
+
+
+def cq_paged_append(k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_cb: torch.Tensor, v_cb: torch.Tensor,
+                    page_table: torch.Tensor, seq_lens: torch.Tensor, c: int, b: int, page_tokens: int, max_q: int, k_pages: torch.Tensor,
+                    v_pages: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    """Codes of new tokens into their pages.  k, v fp16 (n_rows, n_heads, head_dim), laid out like cq_paged_attn's q; k_cb, v_cb fp32
+    (n_heads, G, 2^b, c) as for cq_encode; q_offsets, page_table and seq_lens as for cq_paged_attn (seq_lens counts the new tokens)."""
+    n_rows, n_heads, head_dim = k.shape
+    if tuple(v.shape) != tuple(k.shape):
+        raise ValueError("k and v must have the same shape")
+    for nm, cb in (("k_cb", k_cb), ("v_cb", v_cb)):
+        if tuple(cb.shape) != (n_heads, head_dim // max(c, 1), 1 << b, c):
+            raise ValueError(f"{nm} shape {tuple(cb.shape)} does not match heads/groups/centroids")
+    n_seq, pages_per_seq = page_table.shape
+    if n_rows == 0:
+        return
+    n_pages = _pages(k_pages, v_pages, page_tokens, n_heads, head_dim, c, b)
+    with _one_device(k, v, q_offsets, k_cb, v_cb, page_table, seq_lens, k_pages, v_pages, workspace):
+        workspace = _workspace(workspace, cq_paged_append_workspace_bytes(n_rows, n_heads, head_dim, c, b), k.device)
+        st = lib().cq_paged_append(_dev(k, torch.float16, "k"), _dev(v, torch.float16, "v"), _length(q_offsets, n_seq + 1, "q_offsets"),
+                                   _dev(k_cb, torch.float32, "k_cb"), _dev(v_cb, torch.float32, "v_cb"), _dev(page_table, torch.int32, "page_table"),
+                                   _length(seq_lens, n_seq, "seq_lens"), n_seq, n_rows, max_q, n_heads, head_dim, c, b, n_pages, page_tokens,
+                                   pages_per_seq, _dev(k_pages, torch.uint8, "k_pages"), _dev(v_pages, torch.uint8, "v_pages"),
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    _check(st, "cq_paged_append")
+
+
+def cq_attn_mass_workspace_bytes(n_seq: int, n_q_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, c: int, b: int,
+                                 max_tokens: int) -> int:
+    return int(lib().cq_attn_mass_workspace_bytes(n_seq, n_q_tokens, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens))
+
+
+def cq_attn_mass(q: torch.Tensor, k_codes: torch.Tensor, k_cb: torch.Tensor, seq_lens: torch.Tensor, scale: float, c: int, b: int,
+                 max_tokens: int, mass: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, variant: int = 0) -> torch.Tensor:
+    """Adds the attention weight that every cached token receives from the n_q newest tokens: q fp16 (n_seq, n_q, Hq, head_dim),
+    mass fp32 (n_seq, Hkv, max_tokens) or None (zeros).  Returns mass_out, which may be mass; a mass_out that the call makes is
+    zero behind the lengths."""
+    n_seq, n_q, n_q_heads, head_dim = q.shape
+    n_kv_heads = k_cb.shape[0]
+    shape = (n_seq, n_kv_heads, max_tokens)
+    _hold(cq_codes_bytes(n_seq, max_tokens, n_kv_heads, head_dim, c, b), k_codes=k_codes)
+    with _one_device(q, k_codes, k_cb, seq_lens, mass, mass_out, workspace):
+        if mass is not None:
+            _like(mass, shape, torch.float32, q.device, "mass")
+        mass_out = torch.zeros(shape, dtype=torch.float32, device=q.device) if mass_out is None else _like(mass_out, shape, torch.float32, q.device, "mass_out")
+        workspace = _workspace(workspace, cq_attn_mass_workspace_bytes(n_seq, n_q, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens), q.device)
+        st = lib().cq_attn_mass_variant(_dev(q, torch.float16, "q"), _dev(k_codes, torch.uint8, "k_codes"),
+                                        _book16(k_cb, n_kv_heads, head_dim, c, b, "k_cb"), _length(seq_lens, n_seq, "seq_lens"), float(scale),
+                                        None if mass is None else mass.data_ptr(), n_seq, n_q, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens,
+                                        mass_out.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), variant, _stream())
+    _check(st, "cq_attn_mass")
+    return mass_out
+
+
+def cq_evict(mass: torch.Tensor, k_codes: torch.Tensor, v_codes: torch.Tensor, seq_lens: torch.Tensor, head_dim: int, c: int, b: int,
+             max_tokens: int, n_keep: int, n_sinks: int = 0, n_recent: int = 0, k_codes_out: Optional[torch.Tensor] = None,
+             v_codes_out: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None, out_max_tokens: Optional[int] = None,
+             kept: Optional[torch.Tensor] = None, seq_lens_out: Optional[torch.Tensor] = None):
+    """Keeps, per (sequence, head), the n_sinks first tokens, the n_recent last and the heaviest of the others, n_keep in all; mass fp32
+    (n_seq, n_heads, max_tokens).  In place, or into a cache of capacity out_max_tokens (all three outputs given).  Returns
+    (kept int32 (n_seq, n_heads, n_keep): old positions, -1 behind the last; the new lengths int32 (n_seq,))."""
+    n_seq, n_heads, _ = mass.shape
+    given = [t is not None for t in (k_codes_out, v_codes_out, mass_out)]
+    if any(given) and not all(given):
+        raise ValueError("k_codes_out, v_codes_out and mass_out come together")
+    if not any(given):
+        k_codes_out, v_codes_out, mass_out = k_codes, v_codes, mass
+    room = max_tokens if out_max_tokens is None else out_max_tokens
+    _hold(cq_codes_bytes(n_seq, max_tokens, n_heads, head_dim, c, b), k_codes=k_codes, v_codes=v_codes)
+    _hold(cq_codes_bytes(n_seq, room, n_heads, head_dim, c, b), k_codes_out=k_codes_out, v_codes_out=v_codes_out)
+    with _one_device(mass, k_codes, v_codes, seq_lens, k_codes_out, v_codes_out, mass_out, kept, seq_lens_out):
+        _like(mass, (n_seq, n_heads, max_tokens), torch.float32, mass.device, "mass")
+        _like(mass_out, (n_seq, n_heads, room), torch.float32, mass.device, "mass_out")
+        kept = _like(kept, (n_seq, n_heads, n_keep), torch.int32, mass.device, "kept")
+        seq_lens_out = _like(seq_lens_out, (n_seq,), torch.int32, mass.device, "seq_lens_out")
+        st = lib().cq_evict(mass.data_ptr(), _dev(k_codes, torch.uint8, "k_codes"), _dev(v_codes, torch.uint8, "v_codes"),
+                            _length(seq_lens, n_seq, "seq_lens"), n_seq, n_heads, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, room,
+                            mass_out.data_ptr(), _dev(k_codes_out, torch.uint8, "k_codes_out"), _dev(v_codes_out, torch.uint8, "v_codes_out"),
+                            kept.data_ptr(), seq_lens_out.data_ptr(), _stream())
+    _check(st, "cq_evict")
+    return kept, seq_lens_out

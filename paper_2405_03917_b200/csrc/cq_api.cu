@@ -10,6 +10,7 @@ using namespace cq;
 namespace cq {
 
 namespace {
+constexpr int kMaxHeadDim = 256;
 constexpr int kDeviceSlots = 64, kSmemSlots = 128;
 std::mutex g_device_mutex;
 int g_sm_count[kDeviceSlots] = {};                   // 0: not queried yet
@@ -49,17 +50,6 @@ cudaError_t ensure_dynamic_smem(const void* func, int bytes, int slot)
     return e;
 }
 
-}  // namespace cq
-
-namespace {
-
-constexpr int kMaxHeadDim = 256;
-constexpr int64_t kSmallEncodeVectors = 128;         // appends up to this many vectors per head may take the few-vector kernel
-constexpr int64_t kGenericMaxTableEntries = 24576;   // (G * 2^b) floats x 2 tables must fit shared memory
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Validates the quantiser shape and fills `sh`; n_q_heads == n_kv_heads for encode-side calls.
 int make_shape(int64_t n_seq, int64_t max_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
                Shape* sh)
 {
@@ -86,6 +76,13 @@ int make_shape(int64_t n_seq, int64_t max_tokens, int n_q_heads, int n_kv_heads,
     return CQ_OK;
 }
 
+}  // namespace cq
+
+namespace {
+
+constexpr int64_t kSmallEncodeVectors = 128;         // appends up to this many vectors per head may take the few-vector kernel
+constexpr int64_t kGenericMaxTableEntries = 24576;   // (G * 2^b) floats x 2 tables must fit shared memory
+
 // Partial slots per (sequence, query head) that the workspace must hold for any variant.
 int max_parts(const Shape& sh)
 {
@@ -101,8 +98,6 @@ size_t partial_bytes(const Shape& sh)
 {
     return (size_t)sh.n_seq * sh.n_q_heads * max_parts(sh) * partial_stride(sh.head_dim) * sizeof(float);
 }
-
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 }  // namespace
 

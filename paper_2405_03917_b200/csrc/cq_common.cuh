@@ -67,6 +67,10 @@ __device__ inline int read_code(const uint8_t* __restrict__ block, const Shape& 
 __host__ __device__ inline int partial_stride(int head_dim) { return head_dim + 2; }
 
 // ---- host helpers (cq_api.cu) ----
+// Validates the quantiser shape and fills `sh`; n_q_heads == n_kv_heads for encode-side calls.
+int make_shape(int64_t n_seq, int64_t max_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b, Shape* sh);
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // SM count of the current device (queried once per device and process).
 int device_sm_count();
 // cudaFuncAttributeMaxDynamicSharedMemorySize for `func`, set once per device and (func, bytes);

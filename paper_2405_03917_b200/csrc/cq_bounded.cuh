@@ -80,6 +80,11 @@ cudaError_t launch_mass_plain(const BoundedArgs& a, const float* mass_in, float*
 cudaError_t launch_codes_to_pages(const BoundedArgs& a, const uint8_t* k_staged, const uint8_t* v_staged, uint8_t* k_pages, uint8_t* v_pages,
                                   cudaStream_t st);
 
+// few rows per sequence (cq_gather_attn.cu): head_dim 128, one byte per code, c = 2, 4 or 8
+bool gather_attn_supported(const Shape& sh);
+size_t gather_attn_workspace_bytes();
+cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
+
 // the heaviest tokens of a cache to the front of another (cq_evict.cu)
 struct EvictArgs {
     Shape sh;                          // the cache that is read; n_q_heads == n_kv_heads

@@ -11,6 +11,8 @@ namespace {
 constexpr int64_t kMostTokens = (int64_t)1 << 30;        // positions are 32-bit in these kernels
 constexpr int64_t kMostRows = (int64_t)1 << 30;          // rows x query heads of a call
 
+constexpr int kFewRows = 16;                             // rows (new tokens x R) of a sequence up to which it takes the gather kernel
+
 // What a call shares: the quantiser, the cache, and how many new tokens a sequence may have.
 int bounded_shape(int64_t n_seq, int64_t n_rows, int max_q, int64_t max_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
                   int64_t window, int64_t n_sinks, BoundedArgs* a)
@@ -51,11 +53,14 @@ int status(cudaError_t e) { return e == cudaSuccess ? CQ_OK : CQ_ERR_CUDA; }
 
 int run_attn(const BoundedArgs& a, int variant, void* workspace, size_t workspace_bytes, cudaStream_t st)
 {
-    if (variant < 0 || variant > 1) return CQ_ERR_SHAPE;
+    if (variant < 0 || variant > 2) return CQ_ERR_SHAPE;
+    const bool gather = gather_attn_supported(a.sh);
+    if (variant == 2 && !gather) return CQ_ERR_UNSUPPORTED;
     if (a.n_rows == 0) return CQ_OK;
+    if (variant == 2 || (variant == 0 && gather && (int64_t)a.max_q * a.sh.R <= kFewRows)) return status(launch_gather_attn(a, workspace, st));
     return status(launch_bounded_plain(a, st));
 }
-size_t attn_workspace(const BoundedArgs& a) { return 256; }
+size_t attn_workspace(const BoundedArgs& a) { return gather_attn_supported(a.sh) ? gather_attn_workspace_bytes() : 256; }
 
 }  // namespace
 

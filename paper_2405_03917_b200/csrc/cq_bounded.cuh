@@ -6,6 +6,15 @@
 
 namespace cq {
 
+// Division of block numbers by the blocks of a page: floor(x / d) = floor(x ceil(2^64 / d) / 2^64) for x d < 2^64.
+struct PageDiv {
+    uint64_t inverse = 0;             // 0: d = 1
+    void set(int d) { inverse = d > 1 ? ~(uint64_t)0 / (uint64_t)d + 1 : 0; }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int quotient(int x) const { return inverse ? (int)__umul64hi((uint64_t)x, inverse) : x; }
+#endif
+};
+
 // One call.  sh.max_tokens is the capacity of a sequence, sh.n_blocks its code blocks.  The codes of a contiguous cache are
 // read as pages of the whole capacity, page s being sequence s (page_table null).
 struct BoundedArgs {
@@ -18,6 +27,7 @@ struct BoundedArgs {
     const int32_t* page_table;        // [n_seq][pages_per_seq]
     int64_t n_pages;
     int pages_per_seq, page_blocks;
+    PageDiv page_div;
     int n_rows, max_q;
     int window, sinks;                // window 0: every token up to the query's
     float scale_log2e;
@@ -50,17 +60,24 @@ __device__ __forceinline__ SeqView seq_view(const BoundedArgs& a, int s)
     return v;
 }
 
-// Byte offset of block blk of (sequence s, head h); -1 where the page table names no page.
+// Page that block blk of sequence s lies in (contiguous caches: s itself); -1 where the page table names none.
+__device__ __forceinline__ int page_index(const BoundedArgs& a, int s, int blk)
+{
+    if (!a.page_table) return s;
+    const int page = a.page_table[(int64_t)s * a.pages_per_seq + a.page_div.quotient(blk)];
+    return page >= 0 && page < a.n_pages ? page : -1;
+}
+// Byte offset of block blk of head h, which lies in this page.
+__device__ __forceinline__ int64_t page_block_offset(const BoundedArgs& a, int page, int h, int blk)
+{
+    if (a.page_table) blk -= a.page_div.quotient(blk) * a.page_blocks;
+    return (((int64_t)page * a.sh.n_kv_heads + h) * a.page_blocks + blk) * (int64_t)a.sh.block_bytes;
+}
+// The two in one; -1 without a page.
 __device__ __forceinline__ int64_t block_offset(const BoundedArgs& a, int s, int h, int blk)
 {
-    int64_t page = s;
-    if (a.page_table) {
-        const int at = blk / a.page_blocks;
-        page = a.page_table[(int64_t)s * a.pages_per_seq + at];
-        if (page < 0 || page >= a.n_pages) return -1;
-        blk -= at * a.page_blocks;
-    }
-    return ((page * a.sh.n_kv_heads + h) * a.page_blocks + blk) * (int64_t)a.sh.block_bytes;
+    const int page = page_index(a, s, blk);
+    return page < 0 ? -1 : page_block_offset(a, page, h, blk);
 }
 
 __device__ __forceinline__ bool token_visible(int t, int pos, int window, int sinks)

@@ -45,6 +45,7 @@ int paged_shape(int64_t n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_k
     a->n_pages = n_pages;
     a->pages_per_seq = (int)pages_per_seq;
     a->page_blocks = (int)(page_tokens / kTokenBlock);
+    a->page_div.set(a->page_blocks);
     return CQ_OK;
 }
 

@@ -5,33 +5,43 @@
 // Both codebooks lie in shared memory as fp16, code-major: row j holds the centroids j of all groups (256 bytes).  A warp takes blocks
 // of 16 tokens; its lanes load centroids as they lie there into the fragments of m16n8k16 MMAs, so no tile of keys or values is
 // ever written.  What makes that possible without bank conflicts is the choice of what a fragment's rows and columns mean:
-//   scores: a column of B is (token, half of the groups): the eight lanes that load one token together take eight different groups.
-//       The rows of A hold every query twice, rows r with the channels of one half and rows r + 8 with those of the other, so
-//       that a token's score is the sum of two accumulators of one lane.
+//   scores: a row (four query rows) or a column (eight) of keys is (token, half of the groups): the eight lanes that load one token
+//       together take eight different groups.  The other operand holds every query twice, with the channels of one half and with
+//       those of the other, and the accumulators where the halves agree are added up.
 //   sums:   a loaded word holds two neighbouring channels of ONE token, but the contraction runs over tokens.  So the k pair
 //       (2i, 2i + 1) of an MMA is one token, A's rows r hold (p, 0) there and rows r + 8 (0, p): they sum the even and the odd
 //       channels.  Lanes of a quad hold different tokens of the same column; in the kernel for four rows the rows of A that are left
 //       over select lanes of a quad, so that a column stands for two groups, and a second copy of the value centroids, half a line
 //       further on, parts the rest: no conflict.  With eight rows two lanes meet.
-// Shared memory: 64 KiB + 2 x 64 KiB of centroids, one CTA of 16 warps per SM.
+// Shared memory: 64 KiB + 2 x 64 KiB of centroids, one CTA of eight warps per SM; the codes of a warp's next blocks
+// travel by asynchronous copies.
+//
+// What bounds it: shared memory.  A token costs 4 wavefronts of centroids (of 5 in all) and 3 cycles of MMAs; a block of 16 tokens
+// takes about 115 cycles, 80 of them wavefronts.  64 sequences, 32 heads on 8, CQ-8c8b: window of 4096 81 us, contexts of
+// 4096 ... 16384 in pages 166 us = 1.0 TB/s.
 //
 // Work is dealt evenly: the blocks that all (KV head, sequence, row tile) items attend lie on one line, every CTA takes an equal
 // stretch of it (a stretch that crosses into another KV head loads that head's centroids), and what a cut item leaves behind
 // is merged by a second, small kernel.
+#include <limits.h>
+
 #include "cq_bounded.cuh"
+#include "cq_bulk_copy.cuh"
 
 namespace cq {
 
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32;
 constexpr int kBookBytes = 256 * 256;
-constexpr int kKOffset = 0, kVOffset = kBookBytes, kRedOffset = 3 * kBookBytes;
-constexpr int kRedRegs = 16;                                              // accumulator registers that are reduced at a time
-constexpr int kStatOffset = kRedOffset + kWarps * kRedRegs * 32 * 4;
-constexpr int kSmemBytes = kStatOffset + 2 * kWarps * 8 * 4 + 256;
+constexpr int kKOffset = 0, kVOffset = kBookBytes, kStageOffset = 3 * kBookBytes;
+// Eight warps (12 were as fast: 81 and 82 us for 64 sequences with a window of 4096, 32 heads on 8), and their share of the rest of
+// shared memory: codes on their way (2 blocks' for c = 2, 4 for c = 4, 8 for c = 8), then accumulators.
+constexpr int kWarps = 8, kThreads = kWarps * 32, kWarpBytes = 4096;
+constexpr int kStatOffset = kStageOffset + kWarps * kWarpBytes;           // [warp][8] references, [warp][8] sums, what the scans need
+constexpr int kQOffset = kStatOffset + 2 * kWarps * 8 * 4 + 256;          // queries of the item
+constexpr int kSmemBytes = kQOffset + 8 * 256;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
-constexpr int kLeastShare = 16;                                           // blocks that a CTA takes at least: one per warp
+constexpr int kLeastShare = 16;                                           // blocks that a CTA takes at least
 
 __host__ __device__ constexpr int partial_floats(int rows) { return 2 * rows + (rows == 4 ? 16 : 32) * 32; }
 
@@ -48,9 +58,49 @@ __device__ __forceinline__ float ex2f(float x)
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+
+__device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// prmt with all four selector bits: bit 3 of a nibble puts the sign of the byte it names (zero for a weight's upper byte) into all eight bits
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
+    return d;
+}
+// a centroid's words, as they lie in a code-major codebook
+template <int E>
+__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* at)
+{
+    if (E == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        w[0] = v.x; w[1 % E] = v.y; w[2 % E] = v.z; w[3 % E] = v.w;
+    } else if (E == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        w[0] = v.x; w[1 % E] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(at);
+    }
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copies_wait()      // all but the newest kPending groups
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+}
+__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 
 // Row tiles of a sequence and the blocks that one of them attends at most (at least one: rows that see nothing are written too).
 struct Cost {
@@ -123,25 +173,29 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
     constexpr int kVGroups = kRows == 4 ? 4 / E : 8 / E;                    // groups of a lane's values
     constexpr int kVWords = kRows == 4 ? 2 * kVGroups : kVGroups;           // their code words (eight or four tokens)
     constexpr int kNT = kRows == 4 ? 4 : 8;                                 // accumulator tiles
+    constexpr int kBlockBytes = 2 * G * kTokenBlock;                        // key and value codes of a block
+    constexpr int kStages = kWarpBytes / kBlockBytes;                       // blocks of a warp whose codes have room
+    static_assert(kStages >= 2 && kNT * 4 * 128 <= kWarpBytes, "room");
     extern __shared__ __align__(1024) uint8_t smem[];
-    float* red = reinterpret_cast<float*>(smem + kRedOffset);
-    float* wm = reinterpret_cast<float*>(smem + kStatOffset);               // [warp][8]: reference and sum of the weights
+    float* wm = reinterpret_cast<float*>(smem + kStatOffset);            // [warp][8]: reference and sum of the weights
     float* wl = wm + kWarps * 8;
     int64_t* scratch = reinterpret_cast<int64_t*>(wl + kWarps * 8);
+    uint64_t* book_bar = reinterpret_cast<uint64_t*>(scratch + kWarps);
     const Shape& sh = a.sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = lane >> 2, p = lane & 3, R = sh.R, n_seq = (int)sh.n_seq;
 
     // ---- this CTA's stretch of the line
-    int64_t per_head = 0;
+    int64_t per_head = 0, mine = 0, before = 0;
+    auto blocks_of = [&](int s) {
+        if (s >= n_seq) return (int64_t)0;
+        const Cost c = cost_of<kRows>(a, seq_view(a, s));
+        return (int64_t)c.tiles * c.blocks;
+    };
     for (int s0 = 0; s0 < n_seq; s0 += kThreads) {
-        const int s = s0 + (int)threadIdx.x;
-        int64_t mine = 0, all;
-        if (s < n_seq) {
-            const Cost c = cost_of<kRows>(a, seq_view(a, s));
-            mine = (int64_t)c.tiles * c.blocks;
-        }
-        block_prefix(mine, scratch, all);
+        int64_t all;
+        mine = blocks_of(s0 + (int)threadIdx.x);
+        before = block_prefix(mine, scratch, all);
         per_head += all;
     }
     const int64_t total = per_head * sh.n_kv_heads;
@@ -152,23 +206,21 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
     if (threadIdx.x < 2) cuts[2 * blockIdx.x + threadIdx.x].state = 0;
     if (x >= x_end) return;
     int head = (int)(x / per_head), seq = 0;
-    int64_t rest = x % per_head;                                            // blocks of the sequence before x
+    int64_t rest = x - head * per_head;                                     // blocks of the sequence before x
     for (int s0 = 0; s0 < n_seq; s0 += kThreads) {
-        const int s = s0 + (int)threadIdx.x;
-        int64_t mine = 0, all;
-        if (s < n_seq) {
-            const Cost c = cost_of<kRows>(a, seq_view(a, s));
-            mine = (int64_t)c.tiles * c.blocks;
+        int64_t all = per_head;
+        if (n_seq > kThreads) {                                             // (otherwise the first scan's results are still there)
+            mine = blocks_of(s0 + (int)threadIdx.x);
+            before = block_prefix(mine, scratch, all);
         }
-        const int64_t before = block_prefix(mine, scratch, all);
         if (rest >= all) { rest -= all; continue; }
-        if (before <= rest && rest < before + mine) { scratch[0] = s; scratch[1] = rest - before; }
+        if (before <= rest && rest < before + mine) { scratch[0] = s0 + (int)threadIdx.x; scratch[1] = rest - before; }
         __syncthreads();
         seq = (int)scratch[0];
         rest = scratch[1];
         break;
     }
-    __syncthreads();                                                        // (scratch, and the cut records before their next writers)
+    // (before the next writer of scratch and of the cut records, the CTA has met again)
 
     // a negative scale: the queries change sign instead; a zero one: they become zero; both are exact
     const uint32_t q_sign = a.scale_log2e < 0.f ? 0x80008000u : 0u, q_keep = a.scale_log2e == 0.f ? 0u : 0xffffffffu;
@@ -181,103 +233,224 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
 #pragma unroll
     for (int i = 0; i < kKWords; ++i) koff[i] = (uint32_t)((8 * (i ^ flip) + hp) * 2 * kC);
     uint32_t voff[kVGroups];                                                // the same for values; byte 2: the copy
-    int vgroup[kVGroups];
+    const int vg0 = kRows == 4 ? (r % kLow) * 2 + (p & 1) + 2 * kLow * (r / kLow) : r % kLow + kLow * (r / kLow);       // the first of its groups
 #pragma unroll
     for (int m = 0; m < kVGroups; ++m) {
-        vgroup[m] = kRows == 4 ? (r % kLow) * 2 + (p & 1) + 2 * kLow * (r / kLow + E * m) : r % kLow + kLow * (r / kLow + E * m);
-        voff[m] = (uint32_t)((vgroup[m] * 2 * kC) ^ ((p >> 1) * 64)) | ((uint32_t)(p >> 1) << 16);
+        const int g = vg0 + m * (kRows == 4 ? 2 : 1) * kLow * E;
+        voff[m] = (uint32_t)((g * 2 * kC) ^ ((p >> 1) * 64)) | ((uint32_t)(p >> 1) << 16);
     }
-    const uint32_t smem_base = (uint32_t)__cvta_generic_to_shared(smem);
+    uint8_t* stage0 = smem + kStageOffset + warp * kWarpBytes;              // [stage][block of the turn][key codes, value codes]
+    const uint32_t stage_addr = (uint32_t)__cvta_generic_to_shared(stage0) + 16 * lane;
+    const uint8_t* k_codes = stage0 + hp * kTokenBlock + 4 * tq;            // the lane's codes in a block
+    const uint8_t* v_codes = stage0 + G * kTokenBlock + vg0 * kTokenBlock + (kRows == 4 ? 8 * (p >> 1) : 4 * p);
+    const int64_t from_v = (int64_t)(reinterpret_cast<uintptr_t>(a.vc) - reinterpret_cast<uintptr_t>(a.kc));
+    const uint8_t* src_lane = a.kc + (G == 16 && lane >= 16 ? from_v - 256 : 0) + 16 * lane;      // 16 groups: half a warp per tensor
+    // Weights (packed in twos) to the fragments of the sums: (p, 0), (0, p) of a word's low and of its high half; four rows: in the rows
+    // that select the lane
+    uint32_t sel0 = 0x9910u, sel1 = 0x1099u, sel2 = 0xBB32u, sel3 = 0x32BBu;
+    if (kRows == 4 && (p & 1) != (r >> 2)) sel0 = sel1 = sel2 = sel3 = 0x9999u;
 
-    int loaded = -1;
-    while (x < x_end) {
-        if (loaded != head) {
-            // centroids of the head, code-major; the values twice, the second time with the halves of a 128-byte line exchanged
-            loaded = head;
-            constexpr int kPer = 8 / kC;                                    // centroids of a 16-byte piece
-            constexpr int kSide = 32 / (kC == 8 ? 8 : kC == 4 ? 16 : 32);   // pieces of a group that a warp takes at a time
-            constexpr int kWide = 32 / kSide;                               // groups that it takes at a time
-            const int pieces = sh.K / kPer > 0 ? sh.K / kPer : 1;           // pieces of a group's codebook
-#pragma unroll 1
-            for (int tensor = 0; tensor < 2; ++tensor) {
-                const __half* book = (tensor ? a.vcb : a.kcb) + (int64_t)head * G * sh.K * kC;
-                constexpr int kTasks = (G / kWide) * (256 / kPer / kSide);  // of a warp
-                constexpr int kAhead = 8;
-#pragma unroll 1
-                for (int t0 = warp; t0 < kTasks; t0 += kAhead * kWarps) {
-                    uint4 v[kAhead];
+    // (kept in registers: worked out anew at every use, these cost as much as the rest of the loop)
 #pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const int task = t0 + u * kWarps;
-                        const int g = (task % (G / kWide)) * kWide + lane % kWide, piece = (task / (G / kWide)) * kSide + lane / kWide;
-                        v[u] = make_uint4(0u, 0u, 0u, 0u);
-                        if (task < kTasks && piece < pieces) {
-                            if (sh.K >= kPer) {
-                                v[u] = reinterpret_cast<const uint4*>(book + (int64_t)g * sh.K * kC)[piece];
-                            } else {                                        // two centroids of two channels
-                                const uint2 two = *reinterpret_cast<const uint2*>(book + (int64_t)g * sh.K * kC);
-                                v[u].x = two.x; v[u].y = two.y;
-                            }
-                        }
-                    }
+    for (int i = 0; i < kKWords; ++i) asm volatile("" : "+r"(koff[i]));
 #pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const int task = t0 + u * kWarps;
-                        if (task >= kTasks) break;
-                        const int g = (task % (G / kWide)) * kWide + lane % kWide, piece = (task / (G / kWide)) * kSide + lane / kWide;
-                        const int at = piece * kPer * 256 + g * 2 * kC;
-                        auto put = [&](uint8_t* dst) {
-                            if (kC == 8) *reinterpret_cast<uint4*>(dst) = v[u];
-                            if (kC == 4) {
-                                *reinterpret_cast<uint2*>(dst) = make_uint2(v[u].x, v[u].y);
-                                *reinterpret_cast<uint2*>(dst + 256) = make_uint2(v[u].z, v[u].w);
-                            }
-                            if (kC == 2) {
-                                *reinterpret_cast<uint32_t*>(dst) = v[u].x;
-                                *reinterpret_cast<uint32_t*>(dst + 256) = v[u].y;
-                                *reinterpret_cast<uint32_t*>(dst + 512) = v[u].z;
-                                *reinterpret_cast<uint32_t*>(dst + 768) = v[u].w;
-                            }
-                        };
-                        if (tensor == 0) put(smem + kKOffset + at);
-                        else { put(smem + kVOffset + at); put(smem + kVOffset + kBookBytes + (at ^ 64)); }
-                    }
+    for (int m = 0; m < kVGroups; ++m) asm volatile("" : "+r"(voff[m]));
+    asm volatile("" : "+r"(sel0), "+r"(sel1), "+r"(sel2), "+r"(sel3), "+l"(src_lane));
+
+    // ---- the items of the stretch
+    struct Item {
+        int head, seq, tile, row0, rows;                                    // rows row0 ... of the sequence's (query token, head) rows
+        int q_first, before_q;                                              // the sequence's first row of q; its tokens before the new ones
+        int pos_lo, pos_hi;                                                 // positions of the first and the last row
+        int sb, wb0, xa, v_end;                                             // blocks of sinks, first block of a window, the part of the blocks
+        bool begins, ends;                                                  // whether that part is the item's first, its last
+    };
+    SeqView here = seq_view(a, seq), ahead = here;                          // of the sequence at x, and of the next one
+    auto look_ahead = [&]() { ahead = seq_view(a, seq + 1 == n_seq ? 0 : seq + 1); };
+    auto take = [&](Item& it) {                                             // the item at x; the same in all threads
+        while (x < x_end && head < sh.n_kv_heads) {
+            const SeqView sv = here;
+            const Cost cost = cost_of<kRows>(a, sv);
+            if ((int64_t)cost.tiles * cost.blocks <= rest) {                // the sequence is done (or belongs to another kernel)
+                rest -= (int64_t)cost.tiles * cost.blocks;
+                if (++seq == n_seq) { seq = 0; ++head; }
+                here = ahead;
+                look_ahead();
+                continue;
+            }
+            it.head = head;
+            it.seq = seq;
+            it.tile = (int)(rest / cost.blocks);
+            it.xa = (int)(rest - (int64_t)it.tile * cost.blocks);
+            const int xb = cost.blocks - it.xa < x_end - x ? cost.blocks : it.xa + (int)(x_end - x);
+            it.begins = it.xa == 0;
+            it.ends = xb == cost.blocks;
+            it.row0 = it.tile * kRows;
+            it.rows = sv.m * R - it.row0 < kRows ? sv.m * R - it.row0 : kRows;
+            it.q_first = sv.row0;
+            it.before_q = sv.n - sv.m;
+            it.pos_lo = it.before_q + it.row0 / R;
+            it.pos_hi = it.before_q + (it.row0 + it.rows - 1) / R;
+            // the blocks that some row sees: those of the sinks, then from the first window on
+            it.wb0 = window_first(it.pos_lo, a.window) / kTokenBlock;
+            it.sb = a.window ? (a.sinks + kTokenBlock - 1) / kTokenBlock : 0;
+            it.sb = it.sb < it.wb0 ? it.sb : it.wb0;
+            const int n_blocks = it.pos_hi < 0 ? 0 : it.sb + it.pos_hi / kTokenBlock + 1 - it.wb0;
+            it.v_end = xb < n_blocks ? xb : n_blocks;
+            x += xb - it.xa;
+            rest += xb - it.xa;
+            return true;
+        }
+        return false;
+    };
+    // The warp's i-th block of an item (-1: none), and where it lies (bit 0: some row does not see all of it; -1: nowhere).
+    auto block_of = [&](const Item& it, int i) {
+        const int v = it.xa + warp + i * kWarps;
+        return v >= it.v_end ? -1 : v < it.sb ? v : v - it.sb + it.wb0;
+    };
+    auto look_up = [&](const Item& it, int i) -> int64_t {
+        const int blk = block_of(it, i), t0 = blk * kTokenBlock;
+        if (blk < 0) return -1;
+        const bool all_seen = t0 + kTokenBlock - 1 <= it.pos_lo && (a.window == 0 || t0 > it.pos_hi - a.window || t0 + kTokenBlock <= a.sinks);
+        const int64_t at = block_offset(a, it.seq, it.head, blk);
+        return at < 0 ? -1 : at | (all_seen ? 0 : 1);
+    };
+    auto copy_queries = [&](const Item& it) {                               // (rows beyond the tile's: its last one)
+        if (threadIdx.x < kRows * 16) {
+            const int i = (int)threadIdx.x >> 4, row = it.row0 + (i < it.rows ? i : it.rows - 1);
+            copy16((uint32_t)__cvta_generic_to_shared(smem + kQOffset) + 16 * threadIdx.x,
+                           a.q + (((int64_t)it.q_first + row / R) * sh.n_q_heads + it.head * R + row % R) * 128 + 8 * (threadIdx.x & 15));
+        }
+    };
+    // Centroids of a head: two bulk copies bring them as they lie in memory ([group][code]) into the places of the two value copies;
+    // `lay_out` turns them code-major, the values twice, the second time with the halves of a 128-byte line exchanged.  It goes along
+    // diagonals: the lanes that access shared memory together take different codes of different groups, so that neither side of
+    // the transposition has conflicts.  (Loads that scatter into place cost a tag per 16 bytes: 12 thousand cycles.)
+    constexpr int kKRaw = kVOffset, kVRaw = kVOffset + kBookBytes;
+    uint32_t book_phase = 0u;
+    auto copy_books = [&](int of) {
+        if (threadIdx.x == 0) {
+            const uint32_t bytes = (uint32_t)(G * sh.K * kC) * 2u;
+            fence_async_smem();
+            mbar_expect_tx(book_bar, 2 * bytes);
+            bulk_copy_g2s(smem + kKRaw, a.kcb + (int64_t)of * G * sh.K * kC, bytes, book_bar);
+            bulk_copy_g2s(smem + kVRaw, a.vcb + (int64_t)of * G * sh.K * kC, bytes, book_bar);
+        }
+    };
+    auto lay_out = [&]() -> bool {
+        const bool there = mbar_wait(book_bar, book_phase);
+        if (__syncthreads_or(!there)) {                                     // (a copy that never came: the caller gives up)
+            mbar_wait(book_bar, book_phase);
+            return false;
+        }
+        book_phase ^= 1u;
+        constexpr int kWide = kC == 8 ? 8 : kC == 4 ? 16 : 32;              // lanes that access shared memory together
+        constexpr int kTasks = (G / kWide) * (256 * kWide / 32);            // of a warp: 32 / kWide codes of kWide groups
+        constexpr int kMine = (kTasks + kWarps - 1) / kWarps;
+        auto place = [&](int task, int& from, int& to) {                    // bytes in the raw and in the laid out book; whether there is such a code
+            const int g = (task % (G / kWide)) * kWide + lane % kWide;
+            const int step = (task / (G / kWide)) * (32 / kWide) + lane / kWide;       // of the kWide steps of a square of codes and groups
+            const int j = step / kWide * kWide + (step + lane) % kWide;
+            from = (g * sh.K + j) * 2 * kC;
+            to = j * 256 + g * 2 * kC;
+            return j < sh.K;
+        };
+        auto put = [&](uint8_t* dst, const uint32_t (&w)[E]) {
+            if (E == 4) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1 % E], w[2 % E], w[3 % E]);
+            else if (E == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1 % E]);
+            else *reinterpret_cast<uint32_t*>(dst) = w[0];
+        };
+        uint32_t v[kMine][E];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int task = warp + i * kWarps;
+            if (task >= kTasks) break;
+            int from, to;
+            const bool is = place(task, from, to);
+            uint32_t k[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) k[e] = v[i][e] = 0u;                // (codes of tokens that nobody sees may name these)
+            if (is) {
+                load_words<E>(k, smem + kKRaw + from);
+                load_words<E>(v[i], smem + kVRaw + from);
+            }
+            put(smem + kKOffset + to, k);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int task = warp + i * kWarps;
+            if (task >= kTasks) break;
+            int from, to;
+            place(task, from, to);
+            put(smem + kVOffset + to, v[i]);
+            put(smem + kVOffset + kBookBytes + (to ^ 64), v[i]);
+        }
+        __syncthreads();
+        return true;
+    };
+
+    int loaded = head < sh.n_kv_heads ? head : -1;
+    if (threadIdx.x == 0) {
+        mbar_init(book_bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        copy_books(head);
+    }
+    __syncthreads();
+    look_ahead();
+    Item it, next;
+    bool more = take(it), laid_out = false, broken = false;
+    int64_t where = more ? look_up(it, lane) : -1;                          // lane i: where the i-th of the warp's next 32 blocks lies
+    if (more) copy_queries(it);
+    while (more) {
+        if (loaded != it.head) {
+            loaded = it.head;
+            laid_out = false;
+            copy_books(loaded);
+        }
+        copies_issued();
+        uint32_t partial_now = 0u;                                          // bits of the blocks on their way that need a mask, the oldest lowest
+        auto fetch = [&](int turn) {                                        // starts the copies of a block
+            const int64_t off = __shfl_sync(0xffffffffu, where, turn & 31);
+            const uint32_t dst = stage_addr + (turn % kStages) * kBlockBytes;
+            if (off >= 0) {
+                const uint8_t* src = src_lane + (off & ~(int64_t)1);
+#pragma unroll
+                for (int i = 0; i < kBlockBytes / 512; ++i)
+                    copy16(dst + 512 * i, G == 16 ? src : src + (i < G / 32 ? 512 * i : from_v + 512 * (i - G / 32)));
+            }
+            partial_now |= (uint32_t)(off & 1) << (kStages - 1);
+            copies_issued();
+            if ((turn & 31) == 31) where = look_up(it, turn + 1 + lane);
+        };
+        const int left = it.v_end - it.xa - warp, turns = left <= 0 ? 0 : (left + kWarps - 1) / kWarps;
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) {
+            fetch(i);
+            if (i < kStages - 1) partial_now >>= 1;
+        }
+        if (!laid_out) {
+            copies_wait<kStages>();                                         // the first item's queries
+            broken |= !lay_out();
+            laid_out = true;
+        }
+        // the lane's row of scores: p of four, r of eight (rows beyond the tile's: its last one)
+        constexpr int kQF = kRows == 4 ? 2 : 4;
+        const int my_row = kRows == 4 ? p : r;
+        const int pos = it.before_q + (it.row0 + (my_row < it.rows ? my_row : it.rows - 1)) / R;
+        uint32_t qf[4][kQF];
+        {
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(smem + kQOffset) + (kRows == 4 ? r >> 1 : r) * 64;
+            auto word = [&](int w, int h) { return (qr[(8 * (w / E) + 4 * h + p) * E + w % E] ^ q_sign) & q_keep; };       // w of half h
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (kRows == 4) {
+                    qf[w >> 1][w & 1] = word(w, r & 1);
+                } else {
+                    qf[w >> 1][(2 * (w & 1)) % kQF] = word(w, 0);
+                    qf[w >> 1][(2 * (w & 1) + 1) % kQF] = word(w, 1);
                 }
             }
-            __syncthreads();
-        }
-
-        // ---- the item, and the part of it that lies in the stretch
-        const SeqView sv = seq_view(a, seq);
-        const Cost cost = cost_of<kRows>(a, sv);
-        if ((int64_t)cost.tiles * cost.blocks <= rest) {                    // the sequence is done (or belongs to another kernel)
-            rest -= (int64_t)cost.tiles * cost.blocks;
-            if (++seq == n_seq) { seq = 0; ++head; }
-            if (head >= sh.n_kv_heads) break;
-            continue;
-        }
-        const int tile = (int)(rest / cost.blocks), xa = (int)(rest % cost.blocks);
-        const int xb = cost.blocks - xa < x_end - x ? cost.blocks : xa + (int)(x_end - x);
-        const int row0 = tile * kRows, rows = sv.m * R - row0 < kRows ? sv.m * R - row0 : kRows;
-        const int pos_lo = sv.n - sv.m + row0 / R, pos_hi = sv.n - sv.m + (row0 + rows - 1) / R;      // positions of its first and last row
-        // the blocks that some row sees: those of the sinks, then from the first window on
-        const int wb0 = window_first(pos_lo, a.window) / kTokenBlock;
-        int sb = a.window ? (a.sinks + kTokenBlock - 1) / kTokenBlock : 0;
-        sb = sb < wb0 ? sb : wb0;
-        const int n_blocks = pos_hi < 0 ? 0 : sb + pos_hi / kTokenBlock + 1 - wb0;
-        const int v_end = xb < n_blocks ? xb : n_blocks;
-
-        // this lane's row; rows beyond the tile's do as its last one
-        const int rho = row0 + (kRows == 4 ? r & 3 : r), my_row = rho < row0 + rows ? rho : row0 + rows - 1;
-        const int pos = sv.n - sv.m + my_row / R;
-        uint32_t qa[4][4];
-        {
-            const uint32_t* qr = reinterpret_cast<const uint32_t*>(a.q + (((int64_t)sv.row0 + my_row / R) * sh.n_q_heads + head * R + my_row % R) * 128);
-#pragma unroll
-            for (int w = 0; w < 8; ++w)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    qa[w >> 1][2 * (w & 1) + h] = (qr[(8 * (w / E) + 4 * h + p) * E + w % E] ^ q_sign) & q_keep;
         }
         float acc[kNT][4];
 #pragma unroll
@@ -286,53 +459,14 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
         float m_ref = -INFINITY, l = 0.f;
 
-        uint32_t kw[kKWords], vw[kVWords];
-        int64_t off = -1;
-        auto block_of = [&](int v) { return v < sb ? v : v - sb + wb0; };
-        auto load = [&](int v) {
-            off = v < v_end ? block_offset(a, seq, head, block_of(v)) : -1;
-            const uint8_t *kp = a.kc + off, *vp = a.vc + off;
+        // Scores run one turn ahead of the sums: the two share no register, so that one's loads and products fill the other's waits.
+        auto score = [&](float* sc, const uint8_t* codes) {
+            uint32_t kcur[kKWords];
 #pragma unroll
-            for (int i = 0; i < kKWords; ++i)
-                kw[i] = off >= 0 ? *reinterpret_cast<const uint32_t*>(kp + (8 * (i ^ flip) + hp) * kTokenBlock + 4 * tq) : 0u;
+            for (int i = 0; i < kKWords; ++i) kcur[i] = *reinterpret_cast<const uint32_t*>(codes + 8 * (i ^ flip) * kTokenBlock);
+            auto keys = [&](uint32_t (&w)[8], int j) {                      // words of token 4 tq + j, this lane's groups
 #pragma unroll
-            for (int m = 0; m < kVGroups; ++m) {
-                if (kRows == 4) {
-                    uint2 two = make_uint2(0u, 0u);
-                    if (off >= 0) two = *reinterpret_cast<const uint2*>(vp + vgroup[m] * kTokenBlock + 8 * (p >> 1));
-                    vw[(2 * m) % kVWords] = two.x;
-                    vw[(2 * m + 1) % kVWords] = two.y;
-                } else {
-                    vw[m % kVWords] = off >= 0 ? *reinterpret_cast<const uint32_t*>(vp + vgroup[m] * kTokenBlock + 4 * p) : 0u;
-                }
-            }
-        };
-        load(xa + warp);
-#pragma unroll 1
-        for (int v = xa + warp; v < v_end; v += kWarps) {
-            uint32_t kcur[kKWords], vcur[kVWords];
-#pragma unroll
-            for (int i = 0; i < kKWords; ++i) kcur[i] = kw[i];
-#pragma unroll
-            for (int i = 0; i < kVWords; ++i) vcur[i] = vw[i];
-            const bool here = off >= 0;
-            load(v + kWarps);
-            if (!here) continue;                                            // (the same in all lanes)
-            // ---- scores: this lane's row, tokens 4 p + j of the block
-            float sc[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < kKWords; ++i) {
-                    const uint32_t at = smem_base + kKOffset + __byte_perm(kcur[i], koff[i], 0x7504u | ((uint32_t)j << 4) | 0x0600u);
-                    if (E == 4)
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * (i % 2)]), "=r"(w[4 * (i % 2) + 1]), "=r"(w[4 * (i % 2) + 2]), "=r"(w[4 * (i % 2) + 3]) : "r"(at));
-                    else if (E == 2)
-                        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[2 * (i % 4)]), "=r"(w[2 * (i % 4) + 1]) : "r"(at));
-                    else
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i % 8]) : "r"(at));
-                }
+                for (int i = 0; i < kKWords; ++i) load_words<E>(w + i * E, smem + kKOffset + prmt(kcur[i], koff[i], 0x7704u | ((uint32_t)j << 4)));
                 if (E == 2) {                                               // the eights were loaded in the order of i XOR flip
 #pragma unroll
                     for (int i = 0; i < 4; i += 2)
@@ -354,157 +488,224 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
                                 w[i | bit] = flip & bit ? lo : hi;
                             }
                 }
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
+            };
+            if constexpr (kRows == 4) {
+                float part[4];                                              // over the lane's half of the groups, tokens 4 tq + j
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) mma16816(d, qa[ks][0], qa[ks][1], qa[ks][2], qa[ks][3], w[2 * ks], w[2 * ks + 1]);
-                sc[j] = d[0] + d[3];
+                for (int t = 0; t < 2; ++t) {
+                    uint32_t w0[8], w1[8];
+                    keys(w0, 2 * t);
+                    keys(w1, 2 * t + 1);
+                    float d[4];
+                    mma16816_first(d, w0[0], w1[0], w0[1], w1[1], qf[0][0], qf[0][1]);
+#pragma unroll
+                    for (int ks = 1; ks < 4; ++ks) mma16816(d, w0[2 * ks], w1[2 * ks], w0[2 * ks + 1], w1[2 * ks + 1], qf[ks][0], qf[ks][1]);
+                    part[2 * t] = r & 1 ? d[1] : d[0];
+                    part[2 * t + 1] = r & 1 ? d[3] : d[2];
+                }
+                // the lane of the other half (r ^ 1) keeps the other two tokens
+                const float give0 = r & 1 ? part[0] : part[2], give1 = r & 1 ? part[1] : part[3];
+                sc[0] = (r & 1 ? part[2] : part[0]) + __shfl_xor_sync(0xffffffffu, give0, 4);
+                sc[1] = (r & 1 ? part[3] : part[1]) + __shfl_xor_sync(0xffffffffu, give1, 4);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[8];
+                    keys(w, j);
+                    float d[4];
+                    mma16816_first(d, qf[0][0], qf[0][1], qf[0][2 % kQF], qf[0][3 % kQF], w[0], w[1]);
+#pragma unroll
+                    for (int ks = 1; ks < 4; ++ks) mma16816(d, qf[ks][0], qf[ks][1], qf[ks][2 % kQF], qf[ks][3 % kQF], w[2 * ks], w[2 * ks + 1]);
+                    sc[j] = d[0] + d[3];
+                }
             }
-            const int t0 = block_of(v) * kTokenBlock;
-            const bool all_seen = t0 + kTokenBlock - 1 <= pos_lo && (a.window == 0 || t0 > pos_hi - a.window || t0 + kTokenBlock <= a.sinks);
-            if (!all_seen) {
+        };
+        // Four rows: a lane has the scores of row p, tokens 2 r + {0, 1}; eight: of row r, tokens 4 p + {0 ... 3}.
+        constexpr int kSc = kRows == 4 ? 2 : 4, kX = kRows == 4 ? 4 : 2;
+        uint32_t x[kX];                                                     // weights, in twos, as `sum` takes them
+        auto weigh = [&](float (&sc)[kSc], int turn, uint32_t partial) {
+            if (partial) {
+                // (a block that is not there, or lies in no page: no token)
+                const int blk = block_of(it, turn);
+                const int t0 = blk < 0 || page_index(a, it.seq, blk) < 0 ? INT_MAX - 16 : blk * kTokenBlock + (kRows == 4 ? 2 * r : 4 * p);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!token_visible(t0 + 4 * p + j, pos, a.window, a.sinks)) sc[j] = -INFINITY;
+                for (int j = 0; j < kSc; ++j)
+                    if (!token_visible(t0 + j, pos, a.window, a.sinks)) sc[j] = -INFINITY;
             }
             // ---- weights.  Their reference follows the row's maximum only when it is more than 8 (a factor of 256) behind: fp16
             // weights up to 256 are as precise as weights up to 1, and the sums are rarely rescaled.
-            const float top = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])) * scale;
+            float top = fmaxf(sc[0], sc[1]);
+            if (kSc == 4) top = fmaxf(top, fmaxf(sc[2 % kSc], sc[3 % kSc]));
+            top *= scale;
             if (__any_sync(0xffffffffu, top > m_ref + 8.f)) {
-                float row_top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                row_top = fmaxf(row_top, __shfl_xor_sync(0xffffffffu, row_top, 2));
-                if (row_top > m_ref) {
-                    const float f = m_ref == -INFINITY ? 0.f : ex2f(m_ref - row_top);
-                    m_ref = row_top;
-                    l *= f;
 #pragma unroll
-                    for (int i = 0; i < kNT; ++i)
+                for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float m_new = fmaxf(m_ref, top);
+                float f = m_ref == -INFINITY ? 0.f : ex2f(m_ref - m_new);
+                m_ref = m_new;
+                l *= f;
+                if (kRows == 4) f = __shfl_sync(0xffffffffu, f, r & 3);     // (the accumulators are row r & 3's)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[i][k] *= f;
-                }
+                for (int i = 0; i < kNT; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][k] *= f;
             }
             const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-            uint32_t y[2];
+            uint32_t y[kSc / 2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < kSc / 2; ++j) {
                 const __half2 h = __floats2half2_rn(ex2f(fmaf(sc[2 * j], scale, -ref)), ex2f(fmaf(sc[2 * j + 1], scale, -ref)));
                 const float2 f = __half22float2(h);                         // (the normaliser sums the weights as they are used)
                 l += f.x + f.y;
                 y[j] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            // ---- sums
-            constexpr int kSteps = kRows == 4 ? 4 : 2;                      // a step takes two tokens per lane
-            uint32_t pw[kSteps];
-            if (kRows == 4) {
-                // lanes p and p ^ 1 hold the weights of eight tokens; rows 0-3 use the lanes with even p, rows 4-7 the others
-                const uint32_t z0 = __shfl_xor_sync(0xffffffffu, y[0], 1), z1 = __shfl_xor_sync(0xffffffffu, y[1], 1);
-                const bool active = (p & 1) == (r >> 2), odd = r >> 2;
-                pw[0] = active ? (odd ? z0 : y[0]) : 0u;
-                pw[1] = active ? (odd ? z1 : y[1]) : 0u;
-                pw[2 % kSteps] = active ? (odd ? y[0] : z0) : 0u;
-                pw[3 % kSteps] = active ? (odd ? y[1] : z1) : 0u;
-            } else {
-                pw[0] = y[0];
-                pw[1] = y[1];
+#pragma unroll
+            for (int i = 0; i < kX; ++i) x[i] = kRows == 4 ? __shfl_sync(0xffffffffu, y[0], (2 * (p & 2) + i) * 4 + (r & 3)) : y[i % (kSc / 2)];
+        };
+        // Four rows: row r & 3, tokens 8 (p / 2) + {0 ... 7}; eight: row r, tokens 4 p + {0 ... 3}
+        auto sum = [&](const uint8_t* codes) {
+            uint32_t vcur[kVWords];
+#pragma unroll
+            for (int m = 0; m < kVGroups; ++m) {
+                const uint8_t* at = codes + m * ((kRows == 4 ? 2 : 1) * kLow * E * kTokenBlock);
+                if (kRows == 4) {
+                    const uint2 two = *reinterpret_cast<const uint2*>(at);
+                    vcur[(2 * m) % kVWords] = two.x;
+                    vcur[(2 * m + 1) % kVWords] = two.y;
+                } else {
+                    vcur[m % kVWords] = *reinterpret_cast<const uint32_t*>(at);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const uint32_t a0 = pw[i] & 0xffffu, a1 = pw[i] << 16, a2 = pw[i] >> 16, a3 = pw[i] & 0xffff0000u;
+            for (int i = 0; i < kX; ++i) {
+                const uint32_t a0 = prmt(x[i], x[i], sel0), a1 = prmt(x[i], x[i], sel1), a2 = prmt(x[i], x[i], sel2), a3 = prmt(x[i], x[i], sel3);
 #pragma unroll
                 for (int m = 0; m < kVGroups; ++m) {
-                    uint32_t b[2][4];
+                    uint32_t b[2][E];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const int tok = 2 * i + e;                          // of the lane's four or eight
-                        const uint32_t word = vcur[kRows == 4 ? (2 * m + (tok >> 2)) % kVWords : m % kVWords];
-                        const uint32_t at = smem_base + kVOffset + __byte_perm(word, voff[m], 0x7604u | ((uint32_t)(tok & 3) << 4));
-                        if (E == 4)
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b[e][0]), "=r"(b[e][1]), "=r"(b[e][2]), "=r"(b[e][3]) : "r"(at));
-                        else if (E == 2)
-                            asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(b[e][0]), "=r"(b[e][1]) : "r"(at));
-                        else
-                            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(b[e][0]) : "r"(at));
+                        const int at = 2 * i + e;                           // of the lane's four or eight
+                        const uint32_t word = vcur[kRows == 4 ? (2 * m + (at >> 2)) % kVWords : m % kVWords];
+                        load_words<E>(b[e], smem + kVOffset + prmt(word, voff[m], 0x7604u | ((uint32_t)(at & 3) << 4)));
                     }
 #pragma unroll
                     for (int w = 0; w < E; ++w) mma16816(acc[(m * E + w) % kNT], a0, a1, a2, a3, b[0][w], b[1][w]);
                 }
             }
+        };
+        if (turns > 0) {
+            // Turn i: sums of block i, scores of block i + 1, and the copies of block i + kStages start when its place is free.
+            float sc[kSc];
+            copies_wait<kStages - 1>();
+            __syncwarp();
+            score(sc, k_codes);
+            weigh(sc, 0, partial_now & 1u);
+            partial_now >>= 1;
+#pragma unroll 1
+            for (int turn = 0; turn < turns; ++turn) {
+                copies_wait<kStages - 2>();                                 // those of block turn + 1 are there
+                __syncwarp();
+                score(sc, k_codes + ((turn + 1) % kStages) * kBlockBytes);
+                sum(v_codes + (turn % kStages) * kBlockBytes);
+                weigh(sc, turn + 1, partial_now & 1u);
+                __syncwarp();
+                fetch(turn + kStages);
+                partial_now >>= 1;
+            }
         }
+        copies_wait_all();
+        const bool more_next = take(next);
+        const int64_t where_next = more_next ? look_up(next, lane) : -1;    // (needed when the sums are done)
 
         // ---- the warps' sums to one
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        if (p == 0 && (kRows == 8 || r < 4)) {
-            wm[warp * 8 + r] = m_ref;
-            wl[warp * 8 + r] = l;
-        }
-        const bool whole = xa == 0 && xb == cost.blocks;
-        const int slot = xa == 0;
-        float* part = partials + (int64_t)(2 * blockIdx.x + slot) * partial_floats(kRows);
+        // Every warp brings its accumulators to the largest reference; then they are plain sums.
 #pragma unroll
-        for (int round = 0; round < kNT * 4 / kRedRegs; ++round) {
+        for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        const bool speaks = kRows == 4 ? r == 0 : p == 0;                   // for its row
+        if (speaks) wm[warp * 8 + my_row] = m_ref;
+        __syncthreads();
+        if (more_next) copy_queries(next);                                  // (this item's have been read)
+        float M = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kRedRegs; ++i) red[(warp * kRedRegs + i) * 32 + lane] = acc[(round * kRedRegs + i) >> 2][i & 3];
-            __syncthreads();
-            const int reg = round * kRedRegs + warp;                        // thread (warp, lane) sums register `reg` of lane `lane`
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w * 8 + my_row]);
+        float bring = m_ref == -INFINITY ? 0.f : ex2f(m_ref - M);
+        if (speaks) wl[warp * 8 + my_row] = l * bring;
+        if (kRows == 4) bring = __shfl_sync(0xffffffffu, bring, r & 3);
+        const bool whole = it.begins && it.ends;
+        float* part = partials + (int64_t)(2 * blockIdx.x + (it.begins ? 1 : 0)) * partial_floats(kRows);
+        float* mine = reinterpret_cast<float*>(stage0);
+#pragma unroll
+        for (int i = 0; i < kNT * 4; ++i) mine[i * 32 + lane] = acc[i >> 2][i & 3] * bring;
+        __syncthreads();
+#pragma unroll 2
+        for (int reg = warp; reg < kNT * 4; reg += kWarps) {                // this warp sums one register of all warps, lane by lane
             int row, channel;
             place_of<kC, kRows>(reg, lane, row, channel);
-            float M = -INFINITY, L = 0.f, sum = 0.f;
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w * 8 + row]);
+            float L = 0.f, sum_of = 0.f;
+#pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float mw = wm[w * 8 + row], f = mw == -INFINITY ? 0.f : ex2f(mw - M);
-                L = fmaf(f, wl[w * 8 + row], L);
-                sum = fmaf(f, red[(w * kRedRegs + warp) * 32 + lane], sum);
+                L += wl[w * 8 + row];
+                sum_of += reinterpret_cast<const float*>(smem + kStageOffset + w * kWarpBytes)[reg * 32 + lane];
             }
+            if (broken) sum_of = __int_as_float(0x7fffffff);                // (nothing that could be taken for a result)
             if (whole) {
-                if (row < rows) {
-                    const int at = row0 + row;
-                    a.out[(((int64_t)sv.row0 + at / R) * sh.n_q_heads + head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum / L : 0.f);
+                if (row < it.rows) {
+                    const int at = it.row0 + row;
+                    a.out[(((int64_t)it.q_first + at / R) * sh.n_q_heads + it.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum_of / L : sum_of);
                 }
             } else {
-                part[2 * kRows + reg * 32 + lane] = sum;
-                if (round == 0 && threadIdx.x < 32 && p == 0 && (kRows == 8 || r < 4)) { part[row] = M; part[kRows + row] = L; }
+                part[2 * kRows + reg * 32 + lane] = sum_of;
+                if (reg == 0 && p == 0 && r < kRows) part[kRows + row] = L;
             }
-            __syncthreads();
         }
+        if (!whole && warp == 0 && speaks) part[my_row] = M;
+        copies_wait_all();
+        __syncthreads();
         if (!whole && threadIdx.x == 0) {
             Cut c;
-            c.head = head; c.seq = seq; c.tile = tile; c.state = xb == cost.blocks ? 2 : 1;
-            cuts[2 * blockIdx.x + slot] = c;
+            c.head = it.head; c.seq = it.seq; c.tile = it.tile; c.state = it.ends ? 2 : 1;
+            cuts[2 * blockIdx.x + (it.begins ? 1 : 0)] = c;
         }
-        x += xb - xa;
-        rest += xb - xa;
+        it = next;
+        where = where_next;
+        more = more_next;
     }
+    if (!laid_out) mbar_wait(book_bar, book_phase);                         // (no copy may outlive the CTA)
 }
 
 // CTA k merges the item that begins in CTA k's stretch and goes on in the next ones'.
 template <int kC, int kRows>
-__global__ void __launch_bounds__(kThreads) gather_merge_kernel(BoundedArgs a, const float* __restrict__ partials, const Cut* __restrict__ cuts, int n_ctas)
+__global__ void __launch_bounds__(512) gather_merge_kernel(BoundedArgs a, const float* __restrict__ partials, const Cut* __restrict__ cuts, int n_ctas)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int k = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Cut first = cuts[2 * k + 1];
     if (first.state == 0) return;
-    int last = k + 1;
-    while (last < n_ctas - 1 && cuts[2 * last].state == 1) ++last;
+    int last = k + 1;                                                       // the CTA in whose stretch the item ends
+    for (int j0 = k + 1;; j0 += 32) {
+        const int j = j0 + lane;
+        const uint32_t stop = __ballot_sync(0xffffffffu, j >= n_ctas - 1 || cuts[2 * j].state != 1);
+        if (stop) { last = j0 + __ffs(stop) - 1; break; }
+    }
+    last = last < n_ctas - 1 ? last : n_ctas - 1;
     const SeqView sv = seq_view(a, first.seq);
     const int R = a.sh.R, row0 = first.tile * kRows;
-    for (int reg = warp; reg < (kRows == 4 ? 16 : 32); reg += kWarps) {
+    for (int reg = warp; reg < (kRows == 4 ? 16 : 32); reg += 16) {
         int row, channel;
         place_of<kC, kRows>(reg, lane, row, channel);
+        auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows); };
         float M = -INFINITY, L = 0.f, sum = 0.f;
+#pragma unroll 4
+        for (int j = k; j <= last; ++j) M = fmaxf(M, part(j)[row]);
+#pragma unroll 4
         for (int j = k; j <= last; ++j) {
-            const float* part = partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows);
-            const float mj = part[row], lj = part[kRows + row], xj = part[2 * kRows + reg * 32 + lane];
-            const float m_new = fmaxf(M, mj);
-            if (m_new == -INFINITY) continue;
-            const float fo = ex2f(M - m_new), fj = ex2f(mj - m_new);
-            L = fmaf(L, fo, lj * fj);
-            sum = fmaf(sum, fo, xj * fj);
-            M = m_new;
+            const float mj = part(j)[row], f = mj == -INFINITY ? 0.f : ex2f(mj - M);
+            L = fmaf(f, part(j)[kRows + row], L);
+            sum = fmaf(f, part(j)[2 * kRows + reg * 32 + lane], sum);
         }
         const int at = row0 + row;
         if (at < sv.m * R)
-            a.out[(((int64_t)sv.row0 + at / R) * a.sh.n_q_heads + first.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum / L : 0.f);
+            a.out[(((int64_t)sv.row0 + at / R) * a.sh.n_q_heads + first.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum / L : sum);
     }
 }
 
@@ -521,6 +722,7 @@ cudaError_t launch(const BoundedArgs& a, void* workspace, int slot, cudaStream_t
     e = cudaLaunchKernelEx(&cfg, gather_attn_kernel<kC, kRows>, a, partials, cuts);
     if (e != cudaSuccess) return e;
     cfg.dynamicSmemBytes = 0;
+    cfg.blockDim = dim3(512);
     cfg.gridDim = dim3((unsigned)(grid - 1 > 0 ? grid - 1 : 1));
     return cudaLaunchKernelEx(&cfg, gather_merge_kernel<kC, kRows>, a, (const float*)partials, (const Cut*)cuts, grid);
 }

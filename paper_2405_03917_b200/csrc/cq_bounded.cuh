@@ -102,6 +102,11 @@ bool gather_attn_supported(const Shape& sh);
 size_t gather_attn_workspace_bytes();
 cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
 
+// many rows per sequence (cq_chunk_attn.cu): the tensor-core kernel of the prefill attention in its bounded form
+bool chunk_attn_supported(const Shape& sh);
+size_t chunk_attn_workspace_bytes(const BoundedArgs& a);
+cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
+
 // the heaviest tokens of a cache to the front of another (cq_evict.cu)
 struct EvictArgs {
     Shape sh;                          // the cache that is read; n_q_heads == n_kv_heads

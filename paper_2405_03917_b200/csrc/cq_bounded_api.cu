@@ -52,16 +52,33 @@ int paged_shape(int64_t n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_k
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 int status(cudaError_t e) { return e == cudaSuccess ? CQ_OK : CQ_ERR_CUDA; }
 
-int run_attn(const BoundedArgs& a, int variant, void* workspace, size_t workspace_bytes, cudaStream_t st)
+int run_attn(BoundedArgs a, int variant, void* workspace, cudaStream_t st)
 {
-    if (variant < 0 || variant > 2) return CQ_ERR_SHAPE;
-    const bool gather = gather_attn_supported(a.sh);
-    if (variant == 2 && !gather) return CQ_ERR_UNSUPPORTED;
+    if (variant < 0 || variant > 3) return CQ_ERR_SHAPE;
+    const bool gather = gather_attn_supported(a.sh), chunk = chunk_attn_supported(a.sh);
+    if ((variant == 2 && !gather) || (variant == 3 && !chunk)) return CQ_ERR_UNSUPPORTED;
     if (a.n_rows == 0) return CQ_OK;
-    if (variant == 2 || (variant == 0 && gather && (int64_t)a.max_q * a.sh.R <= kFewRows)) return status(launch_gather_attn(a, workspace, st));
-    return status(launch_bounded_plain(a, st));
+    if (variant == 2) return status(launch_gather_attn(a, workspace, st));
+    if (variant == 3) return status(launch_chunk_attn(a, workspace, st));
+    if (variant == 1 || !gather || !chunk) return status(launch_bounded_plain(a, st));
+    // every sequence takes the kernel of its number of rows; without ragged rows that is the same one for all
+    if ((int64_t)a.max_q * a.sh.R <= kFewRows) return status(launch_gather_attn(a, workspace, st));
+    if (a.q_offsets) {
+        BoundedArgs few = a;
+        few.most_rows = kFewRows;
+        const cudaError_t e = launch_gather_attn(few, workspace, st);
+        if (e != cudaSuccess) return CQ_ERR_CUDA;
+        a.least_rows = kFewRows + 1;
+    }
+    return status(launch_chunk_attn(a, workspace, st));
 }
-size_t attn_workspace(const BoundedArgs& a) { return gather_attn_supported(a.sh) ? gather_attn_workspace_bytes() : 256; }
+size_t attn_workspace(const BoundedArgs& a)
+{
+    size_t bytes = 256;
+    if (gather_attn_supported(a.sh) && gather_attn_workspace_bytes() > bytes) bytes = gather_attn_workspace_bytes();
+    if (chunk_attn_supported(a.sh) && chunk_attn_workspace_bytes(a) > bytes) bytes = chunk_attn_workspace_bytes(a);
+    return bytes;
+}
 
 }  // namespace
 
@@ -97,7 +114,7 @@ int cq_window_attn_variant(const void* q_fp16, const void* k_codes, const void* 
     a.seq_lens = seq_lens;
     a.scale_log2e = scale * kLog2e;
     a.out = static_cast<__half*>(out_fp16);
-    return run_attn(a, variant, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+    return run_attn(a, variant, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int cq_window_attn(const void* q_fp16, const void* k_codes, const void* v_codes, const void* k_cb_fp16, const void* v_cb_fp16,
@@ -142,7 +159,7 @@ int cq_paged_attn_variant(const void* q_fp16, const int32_t* q_offsets, const vo
     a.page_table = page_table;
     a.scale_log2e = scale * kLog2e;
     a.out = static_cast<__half*>(out_fp16);
-    return run_attn(a, variant, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+    return run_attn(a, variant, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int cq_paged_attn(const void* q_fp16, const int32_t* q_offsets, const void* k_pages, const void* v_pages, const void* k_cb_fp16,

@@ -24,7 +24,7 @@ def check_window(case, q, window, sinks, variant, scale=SCALE):
         B.check(out[s], want, tol, f"variant {variant} seq {s} of {n} window {window} sinks {sinks}")
 
 
-VARIANTS = [1, 2]
+VARIANTS = [1, 2, 3]
 
 
 @pytest.mark.parametrize("variant", VARIANTS)

@@ -101,6 +101,9 @@ cudaError_t launch_codes_to_pages(const BoundedArgs& a, const uint8_t* k_staged,
 bool gather_attn_supported(const Shape& sh);
 size_t gather_attn_workspace_bytes();
 cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
+// the masses with the same scores (uniform rows, a contiguous cache, no window); the same shapes
+size_t gather_mass_workspace_bytes(const BoundedArgs& a);
+cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st);
 
 // many rows per sequence (cq_chunk_attn.cu): the tensor-core kernel of the prefill attention in its bounded form
 bool chunk_attn_supported(const Shape& sh);

@@ -207,7 +207,8 @@ size_t cq_attn_mass_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, in
 {
     BoundedArgs a;
     if (bounded_shape(n_seq, (int64_t)n_seq * n_q_tokens, n_q_tokens, max_tokens, n_q_heads, n_kv_heads, head_dim, c, b, 0, 0, &a) != CQ_OK) return 0;
-    return round_up((size_t)a.n_rows * n_q_heads * sizeof(float), 256);
+    const size_t plain = round_up((size_t)a.n_rows * n_q_heads * sizeof(float), 256), tuned = gather_attn_supported(a.sh) ? gather_mass_workspace_bytes(a) : 0;
+    return plain > tuned ? plain : tuned;
 }
 
 int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_cb_fp16, const int32_t* seq_lens, float scale,
@@ -222,12 +223,14 @@ int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_
         !aligned4(mass_out))
         return CQ_ERR_ALIGN;
     if (workspace_bytes < cq_attn_mass_workspace_bytes(n_seq, n_q_tokens, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens)) return CQ_ERR_WORKSPACE;
-    if (variant < 0 || variant > 1) return CQ_ERR_SHAPE;
+    if (variant < 0 || variant > 2) return CQ_ERR_SHAPE;
+    if (variant == 2 && !gather_attn_supported(a.sh)) return CQ_ERR_UNSUPPORTED;
     a.q = static_cast<const __half*>(q_fp16);
     a.kc = static_cast<const uint8_t*>(k_codes);
     a.kcb = static_cast<const __half*>(k_cb_fp16);
     a.seq_lens = seq_lens;
     a.scale_log2e = scale * kLog2e;
+    if (variant != 1 && gather_attn_supported(a.sh)) return status(launch_gather_mass(a, mass_in, mass_out, workspace, static_cast<cudaStream_t>(stream)));
     return status(launch_mass_plain(a, mass_in, mass_out, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }
 

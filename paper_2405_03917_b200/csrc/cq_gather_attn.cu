@@ -1,4 +1,5 @@
-// Attention of few query rows over a coded cache: window, sinks, pages (head_dim 128, one byte per code, c = 2, 4 or 8).
+// Attention of few query rows over a coded cache: window, sinks, pages; and the masses of cached tokens (head_dim 128, one byte per
+// code, c = 2, 4 or 8).
 //
 //   out_r = sum_t p_rt Vhat_t / sum_t p_rt,  p_rt = 2^(scale log2e <q_r, Khat_t> - m_r)      r: (query token, head) of a KV head
 //
@@ -20,6 +21,10 @@
 // takes about 115 cycles, 80 of them wavefronts.  64 sequences, 32 heads on 8, CQ-8c8b: window of 4096 81 us, contexts of
 // 4096 ... 16384 in pages 166 us = 1.0 TB/s.
 //
+// Masses take two passes over the key codes with the same scores: kLse leaves every row's log-sum-exp, kMass turns scores into
+// weights and adds up, per token, those of all rows.  (Row after row tile goes over the same blocks in the same CTA: every sum has one
+// writer and one order.)  They need the key centroids only, so two CTAs share an SM.
+//
 // Work is dealt evenly: the blocks that all (KV head, sequence, row tile) items attend lie on one line, every CTA takes an equal
 // stretch of it (a stretch that crosses into another KV head loads that head's centroids), and what a cut item leaves behind
 // is merged by a second, small kernel.
@@ -32,18 +37,34 @@ namespace cq {
 
 namespace {
 
+enum Mode { kAttn, kLse, kMass };
+
 constexpr int kBookBytes = 256 * 256;
-constexpr int kKOffset = 0, kVOffset = kBookBytes, kStageOffset = 3 * kBookBytes;
 // Eight warps (12 were as fast: 81 and 82 us for 64 sequences with a window of 4096, 32 heads on 8), and their share of the rest of
 // shared memory: codes on their way (2 blocks' for c = 2, 4 for c = 4, 8 for c = 8), then accumulators.
-constexpr int kWarps = 8, kThreads = kWarps * 32, kWarpBytes = 4096;
-constexpr int kStatOffset = kStageOffset + kWarps * kWarpBytes;           // [warp][8] references, [warp][8] sums, what the scans need
-constexpr int kQOffset = kStatOffset + 2 * kWarps * 8 * 4 + 256;          // queries of the item
-constexpr int kSmemBytes = kQOffset + 8 * 256;
-static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kKOffset = 0, kVOffset = kBookBytes;
+template <int kMode>
+struct Cfg {
+    static constexpr int kCtas = kMode == kAttn ? 1 : 2;                      // of an SM
+    static constexpr int kWarpBytes = kMode == kAttn ? 4096 : 2048;
+    static constexpr int kStageOffset = kMode == kAttn ? 3 * kBookBytes : kBookBytes;
+    static constexpr int kStatOffset = kStageOffset + kWarps * kWarpBytes;    // [warp][8] references, [warp][8] sums, what the scans need
+    static constexpr int kQOffset = kStatOffset + 2 * kWarps * 8 * 4 + 256;   // queries of the item, and (kMass) their log-sum-exps
+    static constexpr int kSmemBytes = kQOffset + 8 * 256 + (kMode == kMass ? 32 : 0);
+    static_assert(kSmemBytes <= 227 * 1024 / kCtas - (kCtas > 1 ? 1024 : 0), "shared memory");
+};
 constexpr int kLeastShare = 16;                                           // blocks that a CTA takes at least
 
-__host__ __device__ constexpr int partial_floats(int rows) { return 2 * rows + (rows == 4 ? 16 : 32) * 32; }
+__host__ __device__ constexpr int partial_floats(int rows, int mode) { return 2 * rows + (mode == kAttn ? (rows == 4 ? 16 : 32) * 32 : 0); }
+
+// The masses' part of a call.
+struct MassArgs {
+    const float* mass_in;                                                 // may be null
+    float* mass_out;
+    float* lse;                                                           // [sequence][KV head][row_stride]: log2 of the sum of 2^score
+    int row_stride;
+};
 
 // What a CTA leaves of the items that its stretch cuts: [0] the end or the middle of one, [1] the beginning of one.
 struct Cut {
@@ -106,7 +127,7 @@ __device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_
 struct Cost {
     int tiles, blocks;
 };
-template <int kRows>
+template <int kRows, int kMode>
 __device__ __forceinline__ Cost cost_of(const BoundedArgs& a, const SeqView& v)
 {
     Cost c;
@@ -119,6 +140,10 @@ __device__ __forceinline__ Cost cost_of(const BoundedArgs& a, const SeqView& v)
         c.blocks = c.blocks < most ? c.blocks : (int)most;
     }
     c.blocks = c.blocks < 1 ? 1 : c.blocks;
+    if (kMode == kMass) {                                                   // a CTA goes through all row tiles of its blocks
+        c.blocks = (v.n + kTokenBlock - 1) / kTokenBlock;
+        c.tiles = c.blocks ? 1 : 0;
+    }
     return c;
 }
 
@@ -162,9 +187,12 @@ __device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t* scratch, int
     return before + incl - v;
 }
 
-template <int kC, int kRows>
-__global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a, float* __restrict__ partials, Cut* __restrict__ cuts)
+template <int kC, int kRows, int kMode>
+__global__ void __launch_bounds__(kThreads, Cfg<kMode>::kCtas)
+gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* __restrict__ cuts)
 {
+    using C = Cfg<kMode>;
+    constexpr int kWarpBytes = C::kWarpBytes;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int G = 128 / kC, E = kC / 2;
@@ -173,11 +201,11 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
     constexpr int kVGroups = kRows == 4 ? 4 / E : 8 / E;                    // groups of a lane's values
     constexpr int kVWords = kRows == 4 ? 2 * kVGroups : kVGroups;           // their code words (eight or four tokens)
     constexpr int kNT = kRows == 4 ? 4 : 8;                                 // accumulator tiles
-    constexpr int kBlockBytes = 2 * G * kTokenBlock;                        // key and value codes of a block
+    constexpr int kBlockBytes = (kMode == kAttn ? 2 : 1) * G * kTokenBlock; // key and value codes of a block
     constexpr int kStages = kWarpBytes / kBlockBytes;                       // blocks of a warp whose codes have room
-    static_assert(kStages >= 2 && kNT * 4 * 128 <= kWarpBytes, "room");
+    static_assert(kStages >= 2 && (kMode != kAttn || kNT * 4 * 128 <= kWarpBytes), "room");
     extern __shared__ __align__(1024) uint8_t smem[];
-    float* wm = reinterpret_cast<float*>(smem + kStatOffset);            // [warp][8]: reference and sum of the weights
+    float* wm = reinterpret_cast<float*>(smem + C::kStatOffset);            // [warp][8]: reference and sum of the weights
     float* wl = wm + kWarps * 8;
     int64_t* scratch = reinterpret_cast<int64_t*>(wl + kWarps * 8);
     uint64_t* book_bar = reinterpret_cast<uint64_t*>(scratch + kWarps);
@@ -189,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
     int64_t per_head = 0, mine = 0, before = 0;
     auto blocks_of = [&](int s) {
         if (s >= n_seq) return (int64_t)0;
-        const Cost c = cost_of<kRows>(a, seq_view(a, s));
+        const Cost c = cost_of<kRows, kMode>(a, seq_view(a, s));
         return (int64_t)c.tiles * c.blocks;
     };
     for (int s0 = 0; s0 < n_seq; s0 += kThreads) {
@@ -239,12 +267,12 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
         const int g = vg0 + m * (kRows == 4 ? 2 : 1) * kLow * E;
         voff[m] = (uint32_t)((g * 2 * kC) ^ ((p >> 1) * 64)) | ((uint32_t)(p >> 1) << 16);
     }
-    uint8_t* stage0 = smem + kStageOffset + warp * kWarpBytes;              // [stage][block of the turn][key codes, value codes]
+    uint8_t* stage0 = smem + C::kStageOffset + warp * kWarpBytes;              // [stage][block of the turn][key codes, value codes]
     const uint32_t stage_addr = (uint32_t)__cvta_generic_to_shared(stage0) + 16 * lane;
     const uint8_t* k_codes = stage0 + hp * kTokenBlock + 4 * tq;            // the lane's codes in a block
     const uint8_t* v_codes = stage0 + G * kTokenBlock + vg0 * kTokenBlock + (kRows == 4 ? 8 * (p >> 1) : 4 * p);
     const int64_t from_v = (int64_t)(reinterpret_cast<uintptr_t>(a.vc) - reinterpret_cast<uintptr_t>(a.kc));
-    const uint8_t* src_lane = a.kc + (G == 16 && lane >= 16 ? from_v - 256 : 0) + 16 * lane;      // 16 groups: half a warp per tensor
+    const uint8_t* src_lane = a.kc + (kMode == kAttn && G == 16 && lane >= 16 ? from_v - 256 : 0) + 16 * lane;      // 16 groups: half a warp per tensor
     // Weights (packed in twos) to the fragments of the sums: (p, 0), (0, p) of a word's low and of its high half; four rows: in the rows
     // that select the lane
     uint32_t sel0 = 0x9910u, sel1 = 0x1099u, sel2 = 0xBB32u, sel3 = 0x32BBu;
@@ -259,18 +287,32 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
 
     // ---- the items of the stretch
     struct Item {
-        int head, seq, tile, row0, rows;                                    // rows row0 ... of the sequence's (query token, head) rows
+        int head, seq, tile, tiles, row0, rows;                                  // rows row0 ... of the sequence's (query token, head) rows
         int q_first, before_q;                                              // the sequence's first row of q; its tokens before the new ones
         int pos_lo, pos_hi;                                                 // positions of the first and the last row
-        int sb, wb0, xa, v_end;                                             // blocks of sinks, first block of a window, the part of the blocks
+        int n, sb, wb0, xa, xb, v_end;                                      // tokens; blocks of sinks, first block of a window, the part of the blocks
         bool begins, ends;                                                  // whether that part is the item's first, its last
+    };
+    auto place_tile = [&](Item& it) {                                       // what follows from the number of its row tile
+        it.row0 = it.tile * kRows;
+        it.rows = it.n - it.before_q;                                       // (new tokens)
+        it.rows = it.rows * R - it.row0 < kRows ? it.rows * R - it.row0 : kRows;
+        it.pos_lo = it.before_q + it.row0 / R;
+        it.pos_hi = it.before_q + (it.row0 + it.rows - 1) / R;
+        // the blocks that some row sees: those of the sinks, then from the first window on
+        it.wb0 = window_first(it.pos_lo, a.window) / kTokenBlock;
+        it.sb = a.window ? (a.sinks + kTokenBlock - 1) / kTokenBlock : 0;
+        it.sb = it.sb < it.wb0 ? it.sb : it.wb0;
+        const int last = kMode == kMass && it.tile == 0 ? it.n - 1 : it.pos_hi;      // (masses: the first tile takes what was there along)
+        const int n_blocks = last < 0 ? 0 : it.sb + last / kTokenBlock + 1 - it.wb0;
+        it.v_end = it.xb < n_blocks ? it.xb : n_blocks;
     };
     SeqView here = seq_view(a, seq), ahead = here;                          // of the sequence at x, and of the next one
     auto look_ahead = [&]() { ahead = seq_view(a, seq + 1 == n_seq ? 0 : seq + 1); };
     auto take = [&](Item& it) {                                             // the item at x; the same in all threads
         while (x < x_end && head < sh.n_kv_heads) {
             const SeqView sv = here;
-            const Cost cost = cost_of<kRows>(a, sv);
+            const Cost cost = cost_of<kRows, kMode>(a, sv);
             if ((int64_t)cost.tiles * cost.blocks <= rest) {                // the sequence is done (or belongs to another kernel)
                 rest -= (int64_t)cost.tiles * cost.blocks;
                 if (++seq == n_seq) { seq = 0; ++head; }
@@ -281,22 +323,16 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             it.head = head;
             it.seq = seq;
             it.tile = (int)(rest / cost.blocks);
+            it.tiles = (sv.m * R + kRows - 1) / kRows;
             it.xa = (int)(rest - (int64_t)it.tile * cost.blocks);
             const int xb = cost.blocks - it.xa < x_end - x ? cost.blocks : it.xa + (int)(x_end - x);
             it.begins = it.xa == 0;
             it.ends = xb == cost.blocks;
-            it.row0 = it.tile * kRows;
-            it.rows = sv.m * R - it.row0 < kRows ? sv.m * R - it.row0 : kRows;
             it.q_first = sv.row0;
             it.before_q = sv.n - sv.m;
-            it.pos_lo = it.before_q + it.row0 / R;
-            it.pos_hi = it.before_q + (it.row0 + it.rows - 1) / R;
-            // the blocks that some row sees: those of the sinks, then from the first window on
-            it.wb0 = window_first(it.pos_lo, a.window) / kTokenBlock;
-            it.sb = a.window ? (a.sinks + kTokenBlock - 1) / kTokenBlock : 0;
-            it.sb = it.sb < it.wb0 ? it.sb : it.wb0;
-            const int n_blocks = it.pos_hi < 0 ? 0 : it.sb + it.pos_hi / kTokenBlock + 1 - it.wb0;
-            it.v_end = xb < n_blocks ? xb : n_blocks;
+            it.n = sv.n;
+            it.xb = xb;
+            place_tile(it);
             x += xb - it.xa;
             rest += xb - it.xa;
             return true;
@@ -318,23 +354,27 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
     auto copy_queries = [&](const Item& it) {                               // (rows beyond the tile's: its last one)
         if (threadIdx.x < kRows * 16) {
             const int i = (int)threadIdx.x >> 4, row = it.row0 + (i < it.rows ? i : it.rows - 1);
-            copy16((uint32_t)__cvta_generic_to_shared(smem + kQOffset) + 16 * threadIdx.x,
+            copy16((uint32_t)__cvta_generic_to_shared(smem + C::kQOffset) + 16 * threadIdx.x,
                            a.q + (((int64_t)it.q_first + row / R) * sh.n_q_heads + it.head * R + row % R) * 128 + 8 * (threadIdx.x & 15));
         }
+        if (kMode == kMass && threadIdx.x < kRows / 4)
+            copy16((uint32_t)__cvta_generic_to_shared(smem + C::kQOffset) + 2048 + 16 * threadIdx.x,
+                   mass.lse + ((int64_t)it.seq * sh.n_kv_heads + it.head) * mass.row_stride + it.row0 + 4 * threadIdx.x);
     };
     // Centroids of a head: two bulk copies bring them as they lie in memory ([group][code]) into the places of the two value copies;
     // `lay_out` turns them code-major, the values twice, the second time with the halves of a 128-byte line exchanged.  It goes along
     // diagonals: the lanes that access shared memory together take different codes of different groups, so that neither side of
     // the transposition has conflicts.  (Loads that scatter into place cost a tag per 16 bytes: 12 thousand cycles.)
-    constexpr int kKRaw = kVOffset, kVRaw = kVOffset + kBookBytes;
+    // (Without values the keys are turned in place.)
+    constexpr int kKRaw = kMode == kAttn ? kVOffset : kKOffset, kVRaw = kVOffset + kBookBytes;
     uint32_t book_phase = 0u;
     auto copy_books = [&](int of) {
         if (threadIdx.x == 0) {
             const uint32_t bytes = (uint32_t)(G * sh.K * kC) * 2u;
             fence_async_smem();
-            mbar_expect_tx(book_bar, 2 * bytes);
+            mbar_expect_tx(book_bar, kMode == kAttn ? 2 * bytes : bytes);
             bulk_copy_g2s(smem + kKRaw, a.kcb + (int64_t)of * G * sh.K * kC, bytes, book_bar);
-            bulk_copy_g2s(smem + kVRaw, a.vcb + (int64_t)of * G * sh.K * kC, bytes, book_bar);
+            if (kMode == kAttn) bulk_copy_g2s(smem + kVRaw, a.vcb + (int64_t)of * G * sh.K * kC, bytes, book_bar);
         }
     };
     auto lay_out = [&]() -> bool {
@@ -370,11 +410,9 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             uint32_t k[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) k[e] = v[i][e] = 0u;                // (codes of tokens that nobody sees may name these)
-            if (is) {
-                load_words<E>(k, smem + kKRaw + from);
-                load_words<E>(v[i], smem + kVRaw + from);
-            }
-            put(smem + kKOffset + to, k);
+            if (is && kMode == kAttn) load_words<E>(k, smem + kKRaw + from);
+            if (is) load_words<E>(v[i], smem + (kMode == kAttn ? kVRaw : kKRaw) + from);
+            if (kMode == kAttn) put(smem + kKOffset + to, k);
         }
         __syncthreads();
 #pragma unroll
@@ -383,8 +421,8 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             if (task >= kTasks) break;
             int from, to;
             place(task, from, to);
-            put(smem + kVOffset + to, v[i]);
-            put(smem + kVOffset + kBookBytes + (to ^ 64), v[i]);
+            put(smem + (kMode == kAttn ? kVOffset : kKOffset) + to, v[i]);
+            if (kMode == kAttn) put(smem + kVOffset + kBookBytes + (to ^ 64), v[i]);
         }
         __syncthreads();
         return true;
@@ -415,9 +453,13 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             const uint32_t dst = stage_addr + (turn % kStages) * kBlockBytes;
             if (off >= 0) {
                 const uint8_t* src = src_lane + (off & ~(int64_t)1);
+                if (kMode != kAttn && G == 16) {
+                    if (lane < 16) copy16(dst, src);
+                } else {
 #pragma unroll
-                for (int i = 0; i < kBlockBytes / 512; ++i)
-                    copy16(dst + 512 * i, G == 16 ? src : src + (i < G / 32 ? 512 * i : from_v + 512 * (i - G / 32)));
+                    for (int i = 0; i < kBlockBytes / 512; ++i)
+                        copy16(dst + 512 * i, G == 16 ? src : src + (i < G / 32 ? 512 * i : from_v + 512 * (i - G / 32)));
+                }
             }
             partial_now |= (uint32_t)(off & 1) << (kStages - 1);
             copies_issued();
@@ -440,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
         const int pos = it.before_q + (it.row0 + (my_row < it.rows ? my_row : it.rows - 1)) / R;
         uint32_t qf[4][kQF];
         {
-            const uint32_t* qr = reinterpret_cast<const uint32_t*>(smem + kQOffset) + (kRows == 4 ? r >> 1 : r) * 64;
+            const uint32_t* qr = reinterpret_cast<const uint32_t*>(smem + C::kQOffset) + (kRows == 4 ? r >> 1 : r) * 64;
             auto word = [&](int w, int h) { return (qr[(8 * (w / E) + 4 * h + p) * E + w % E] ^ q_sign) & q_keep; };       // w of half h
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
@@ -457,7 +499,24 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
         for (int i = 0; i < kNT; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
-        float m_ref = -INFINITY, l = 0.f;
+        float m_ref = -INFINITY, l = 0.f;                                   // kMass: m_ref is the row's log-sum-exp
+        float* sums = nullptr;
+        float was[kRows == 4 ? 2 : 4];                                      // sums so far of the tokens that are weighed next
+        auto look_back = [&](int turn) {
+            if constexpr (kMode == kMass) {
+                const int blk = block_of(it, turn), t0 = blk * kTokenBlock + (kRows == 4 ? 2 * r : 4 * p);
+#pragma unroll
+                for (int j = 0; j < (kRows == 4 ? 2 : 4); ++j) {
+                    was[j] = 0.f;
+                    if (blk >= 0 && (kRows == 4 ? p : r) == 0 && t0 + j < it.n && (it.tile > 0 || mass.mass_in))
+                        was[j] = it.tile > 0 ? sums[t0 + j] : mass.mass_in[(sums - mass.mass_out) + t0 + j];
+                }
+            }
+        };
+        if constexpr (kMode == kMass) {
+            m_ref = reinterpret_cast<const float*>(smem + C::kQOffset + 2048)[my_row];
+            sums = mass.mass_out + ((int64_t)it.seq * sh.n_kv_heads + it.head) * sh.max_tokens;
+        }
 
         // Scores run one turn ahead of the sums: the two share no register, so that one's loads and products fill the other's waits.
         auto score = [&](float* sc, const uint8_t* codes) {
@@ -534,6 +593,21 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             }
             // ---- weights.  Their reference follows the row's maximum only when it is more than 8 (a factor of 256) behind: fp16
             // weights up to 256 are as precise as weights up to 1, and the sums are rarely rescaled.
+            if constexpr (kMode == kMass) {
+                // the rows' weights of a token add up across the lanes that hold them; one lane of them has the sum so far
+                float w[kSc];
+#pragma unroll
+                for (int j = 0; j < kSc; ++j) {
+                    w[j] = my_row < it.rows && sc[j] != -INFINITY ? ex2f(fmaf(sc[j], scale, -m_ref)) : 0.f;      // (a row that sees nothing: -inf)
+#pragma unroll
+                    for (int o = kRows == 4 ? 1 : 4; o <= (kRows == 4 ? 2 : 16); o <<= 1) w[j] += __shfl_xor_sync(0xffffffffu, w[j], o);
+                }
+                const int blk = block_of(it, turn), t0 = blk * kTokenBlock + (kRows == 4 ? 2 * r : 4 * p);
+                if (blk >= 0 && (kRows == 4 ? p : r) == 0)
+#pragma unroll
+                    for (int j = 0; j < kSc; ++j)
+                        if (t0 + j < it.n) sums[t0 + j] = was[j] + (broken ? __int_as_float(0x7fffffff) : w[j]);
+            } else {
             float top = fmaxf(sc[0], sc[1]);
             if (kSc == 4) top = fmaxf(top, fmaxf(sc[2 % kSc], sc[3 % kSc]));
             top *= scale;
@@ -544,13 +618,19 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
                 float f = m_ref == -INFINITY ? 0.f : ex2f(m_ref - m_new);
                 m_ref = m_new;
                 l *= f;
-                if (kRows == 4) f = __shfl_sync(0xffffffffu, f, r & 3);     // (the accumulators are row r & 3's)
+                if constexpr (kMode == kAttn) {
+                    if (kRows == 4) f = __shfl_sync(0xffffffffu, f, r & 3); // (the accumulators are row r & 3's)
 #pragma unroll
-                for (int i = 0; i < kNT; ++i)
+                    for (int i = 0; i < kNT; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][k] *= f;
+                        for (int k = 0; k < 4; ++k) acc[i][k] *= f;
+                }
             }
             const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+            if constexpr (kMode == kLse) {
+#pragma unroll
+                for (int j = 0; j < kSc; ++j) l += ex2f(fmaf(sc[j], scale, -ref));
+            } else {
             uint32_t y[kSc / 2];
 #pragma unroll
             for (int j = 0; j < kSc / 2; ++j) {
@@ -561,6 +641,8 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             }
 #pragma unroll
             for (int i = 0; i < kX; ++i) x[i] = kRows == 4 ? __shfl_sync(0xffffffffu, y[0], (2 * (p & 2) + i) * 4 + (r & 3)) : y[i % (kSc / 2)];
+            }
+            }
         };
         // Four rows: row r & 3, tokens 8 (p / 2) + {0 ... 7}; eight: row r, tokens 4 p + {0 ... 3}
         auto sum = [&](const uint8_t* codes) {
@@ -598,6 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             float sc[kSc];
             copies_wait<kStages - 1>();
             __syncwarp();
+            look_back(0);
             score(sc, k_codes);
             weigh(sc, 0, partial_now & 1u);
             partial_now >>= 1;
@@ -605,8 +688,9 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             for (int turn = 0; turn < turns; ++turn) {
                 copies_wait<kStages - 2>();                                 // those of block turn + 1 are there
                 __syncwarp();
+                look_back(turn + 1);
                 score(sc, k_codes + ((turn + 1) % kStages) * kBlockBytes);
-                sum(v_codes + (turn % kStages) * kBlockBytes);
+                if constexpr (kMode == kAttn) sum(v_codes + (turn % kStages) * kBlockBytes);
                 weigh(sc, turn + 1, partial_now & 1u);
                 __syncwarp();
                 fetch(turn + kStages);
@@ -614,9 +698,22 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             }
         }
         copies_wait_all();
-        const bool more_next = take(next);
+        bool more_next = true;
+        if (kMode == kMass && it.tile + 1 < it.tiles) {
+            next = it;
+            ++next.tile;
+            place_tile(next);
+        } else {
+            more_next = take(next);
+        }
         const int64_t where_next = more_next ? look_up(next, lane) : -1;    // (needed when the sums are done)
 
+        if constexpr (kMode == kMass) {
+            __syncthreads();
+            if (more_next) copy_queries(next);                              // (this item's have been read)
+            copies_wait_all();
+            __syncthreads();
+        } else {
         // ---- the warps' sums to one
         // Every warp brings its accumulators to the largest reference; then they are plain sums.
 #pragma unroll
@@ -632,7 +729,26 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
         if (speaks) wl[warp * 8 + my_row] = l * bring;
         if (kRows == 4) bring = __shfl_sync(0xffffffffu, bring, r & 3);
         const bool whole = it.begins && it.ends;
-        float* part = partials + (int64_t)(2 * blockIdx.x + (it.begins ? 1 : 0)) * partial_floats(kRows);
+        float* part = partials + (int64_t)(2 * blockIdx.x + (it.begins ? 1 : 0)) * partial_floats(kRows, kMode);
+        if constexpr (kMode == kLse) {
+            __syncthreads();
+            if (threadIdx.x < kRows) {                                      // (the first lane of a row's lanes holds the largest reference)
+                float L = 0.f, top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    L += wl[w * 8 + threadIdx.x];
+                    top = fmaxf(top, wm[w * 8 + threadIdx.x]);
+                }
+                if (broken) L = __int_as_float(0x7fffffff);
+                if (!whole) {
+                    part[threadIdx.x] = top;
+                    part[kRows + threadIdx.x] = L;
+                } else if ((int)threadIdx.x < it.rows) {
+                    mass.lse[((int64_t)it.seq * sh.n_kv_heads + it.head) * mass.row_stride + it.row0 + threadIdx.x] = top + log2f(L);
+                }
+            }
+        }
+        if constexpr (kMode == kAttn) {
         float* mine = reinterpret_cast<float*>(stage0);
 #pragma unroll
         for (int i = 0; i < kNT * 4; ++i) mine[i * 32 + lane] = acc[i >> 2][i & 3] * bring;
@@ -645,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 L += wl[w * 8 + row];
-                sum_of += reinterpret_cast<const float*>(smem + kStageOffset + w * kWarpBytes)[reg * 32 + lane];
+                sum_of += reinterpret_cast<const float*>(smem + C::kStageOffset + w * kWarpBytes)[reg * 32 + lane];
             }
             if (broken) sum_of = __int_as_float(0x7fffffff);                // (nothing that could be taken for a result)
             if (whole) {
@@ -659,12 +775,14 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
             }
         }
         if (!whole && warp == 0 && speaks) part[my_row] = M;
+        }
         copies_wait_all();
         __syncthreads();
         if (!whole && threadIdx.x == 0) {
             Cut c;
             c.head = it.head; c.seq = it.seq; c.tile = it.tile; c.state = it.ends ? 2 : 1;
             cuts[2 * blockIdx.x + (it.begins ? 1 : 0)] = c;
+        }
         }
         it = next;
         where = where_next;
@@ -674,8 +792,9 @@ __global__ void __launch_bounds__(kThreads, 1) gather_attn_kernel(BoundedArgs a,
 }
 
 // CTA k merges the item that begins in CTA k's stretch and goes on in the next ones'.
-template <int kC, int kRows>
-__global__ void __launch_bounds__(512) gather_merge_kernel(BoundedArgs a, const float* __restrict__ partials, const Cut* __restrict__ cuts, int n_ctas)
+template <int kC, int kRows, int kMode>
+__global__ void __launch_bounds__(kMode == kAttn ? 512 : 32)
+gather_merge_kernel(BoundedArgs a, MassArgs mass, const float* __restrict__ partials, const Cut* __restrict__ cuts, int n_ctas)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int k = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -690,10 +809,20 @@ __global__ void __launch_bounds__(512) gather_merge_kernel(BoundedArgs a, const 
     last = last < n_ctas - 1 ? last : n_ctas - 1;
     const SeqView sv = seq_view(a, first.seq);
     const int R = a.sh.R, row0 = first.tile * kRows;
+    if constexpr (kMode == kLse) {
+        if (lane >= kRows || row0 + lane >= sv.m * R) return;
+        auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows, kMode) + lane; };
+        float M = -INFINITY, L = 0.f;
+#pragma unroll 4
+        for (int j = k; j <= last; ++j) M = fmaxf(M, part(j)[0]);
+#pragma unroll 4
+        for (int j = k; j <= last; ++j) L = fmaf(part(j)[0] == -INFINITY ? 0.f : ex2f(part(j)[0] - M), part(j)[kRows], L);
+        mass.lse[((int64_t)first.seq * a.sh.n_kv_heads + first.head) * mass.row_stride + row0 + lane] = M + log2f(L);
+    } else {
     for (int reg = warp; reg < (kRows == 4 ? 16 : 32); reg += 16) {
         int row, channel;
         place_of<kC, kRows>(reg, lane, row, channel);
-        auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows); };
+        auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows, kMode); };
         float M = -INFINITY, L = 0.f, sum = 0.f;
 #pragma unroll 4
         for (int j = k; j <= last; ++j) M = fmaxf(M, part(j)[row]);
@@ -707,43 +836,66 @@ __global__ void __launch_bounds__(512) gather_merge_kernel(BoundedArgs a, const 
         if (at < sv.m * R)
             a.out[(((int64_t)sv.row0 + at / R) * a.sh.n_q_heads + first.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum / L : sum);
     }
+    }
 }
 
-template <int kC, int kRows>
-cudaError_t launch(const BoundedArgs& a, void* workspace, int slot, cudaStream_t st)
+template <int kC, int kRows, int kMode>
+cudaError_t launch(const BoundedArgs& a, const MassArgs& mass, void* workspace, int slot, cudaStream_t st)
 {
-    const int grid = device_sm_count();
+    using C = Cfg<kMode>;
+    const int grid = device_sm_count() * C::kCtas;
     Cut* cuts = static_cast<Cut*>(workspace);
     float* partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(2 * grid * sizeof(Cut), 256));
-    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(gather_attn_kernel<kC, kRows>), kSmemBytes, slot);
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(gather_kernel<kC, kRows, kMode>), C::kSmemBytes, slot);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr;
-    cudaLaunchConfig_t cfg = overlapped_config((unsigned)grid, kThreads, kSmemBytes, st, &attr);
-    e = cudaLaunchKernelEx(&cfg, gather_attn_kernel<kC, kRows>, a, partials, cuts);
-    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = overlapped_config((unsigned)grid, kThreads, C::kSmemBytes, st, &attr);
+    e = cudaLaunchKernelEx(&cfg, gather_kernel<kC, kRows, kMode>, a, mass, partials, cuts);
+    if (e != cudaSuccess || kMode == kMass) return e;
     cfg.dynamicSmemBytes = 0;
-    cfg.blockDim = dim3(512);
+    cfg.blockDim = dim3(kMode == kAttn ? 512 : 32);
     cfg.gridDim = dim3((unsigned)(grid - 1 > 0 ? grid - 1 : 1));
-    return cudaLaunchKernelEx(&cfg, gather_merge_kernel<kC, kRows>, a, (const float*)partials, (const Cut*)cuts, grid);
+    return cudaLaunchKernelEx(&cfg, gather_merge_kernel<kC, kRows, kMode>, a, mass, (const float*)partials, (const Cut*)cuts, grid);
+}
+
+size_t cuts_bytes(int mode) { return round_up(2 * (size_t)device_sm_count() * (mode == kAttn ? 1 : 2) * sizeof(Cut), 256); }
+size_t gather_bytes(int mode)
+{
+    return cuts_bytes(mode) + round_up(2 * (size_t)device_sm_count() * (mode == kAttn ? 1 : 2) * partial_floats(8, mode) * sizeof(float), 256);
+}
+int mass_row_stride(const BoundedArgs& a) { return (a.max_q * a.sh.R + 7) / 8 * 8; }
+
+template <int kMode>
+cudaError_t launch_mode(const BoundedArgs& a, const MassArgs& mass, void* workspace, int slot, cudaStream_t st)
+{
+    // Tiles of four rows where a query token has that few heads, otherwise of eight: with four rows no two lanes meet in a bank.
+    // (Masses of many rows go over the keys once per tile: eight rows at a time from 16 rows on.)
+    const bool four = kMode == kAttn ? a.sh.R <= 4 : a.max_q * a.sh.R <= 4;
+    if (a.sh.c == 8) return four ? launch<8, 4, kMode>(a, mass, workspace, slot, st) : launch<8, 8, kMode>(a, mass, workspace, slot + 1, st);
+    if (a.sh.c == 4) return four ? launch<4, 4, kMode>(a, mass, workspace, slot + 2, st) : launch<4, 8, kMode>(a, mass, workspace, slot + 3, st);
+    return four ? launch<2, 4, kMode>(a, mass, workspace, slot + 4, st) : launch<2, 8, kMode>(a, mass, workspace, slot + 5, st);
 }
 
 }  // namespace
 
 bool gather_attn_supported(const Shape& sh) { return sh.head_dim == 128 && sh.b <= 8 && (sh.c == 2 || sh.c == 4 || sh.c == 8); }
 
-size_t gather_attn_workspace_bytes()
-{
-    const size_t grid = (size_t)device_sm_count();
-    return round_up(2 * grid * sizeof(Cut), 256) + round_up(2 * grid * partial_floats(8) * sizeof(float), 256);
-}
+size_t gather_attn_workspace_bytes() { return gather_bytes(kAttn); }
+cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st) { return launch_mode<kAttn>(a, MassArgs(), workspace, 100, st); }
 
-// Tiles of four rows where a query token has that few heads, otherwise of eight: with four rows no two lanes meet in a bank.
-cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st)
+size_t gather_mass_workspace_bytes(const BoundedArgs& a)
 {
-    const bool four = a.sh.R <= 4;
-    if (a.sh.c == 8) return four ? launch<8, 4>(a, workspace, 100, st) : launch<8, 8>(a, workspace, 101, st);
-    if (a.sh.c == 4) return four ? launch<4, 4>(a, workspace, 102, st) : launch<4, 8>(a, workspace, 103, st);
-    return four ? launch<2, 4>(a, workspace, 104, st) : launch<2, 8>(a, workspace, 105, st);
+    return gather_bytes(kLse) + round_up((size_t)a.sh.n_seq * a.sh.n_kv_heads * mass_row_stride(a) * sizeof(float), 256);
+}
+cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st)
+{
+    MassArgs mass;
+    mass.mass_in = mass_in;
+    mass.mass_out = mass_out;
+    mass.lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + gather_bytes(kLse));
+    mass.row_stride = mass_row_stride(a);
+    const cudaError_t e = launch_mode<kLse>(a, mass, workspace, 109, st);
+    return e != cudaSuccess ? e : launch_mode<kMass>(a, mass, workspace, 115, st);
 }
 
 }  // namespace cq

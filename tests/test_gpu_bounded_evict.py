@@ -9,7 +9,7 @@ from tests import bounded as B
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 SCALE = 128 ** -0.5
-VARIANTS = [1]
+VARIANTS = [1, 2]
 
 
 def mass_tolerance(case, s, q, n, p):

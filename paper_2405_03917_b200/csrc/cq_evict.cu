@@ -3,9 +3,12 @@
 // Per (sequence, head): of n cached tokens stay the n_sinks first, the n_recent last and, of the others, those of largest mass
 // (equal masses: the lower position), n_keep in all; codes and masses move to positions 0, 1, ... in their old order.
 //
-//   evict_select_kernel  one CTA per (sequence, head): the masses become whole numbers of the same order, the n-th largest is
-//       found by three histograms of 11, 11 and 10 bits in shared memory, and the positions that stay are listed in order
-//       (ballots in a warp, one scan over the warps).
+//   evict_select_kernel  one CTA per (sequence, head): the masses become whole numbers of the same order, kept in registers.  The
+//       last one that stays is found by two histograms of 8 bits in shared memory; the few tokens that share these 16 bits with it are
+//       then ranked against each other, and the positions that stay are listed in order (ballots in a warp, one scan over the warps).
+//       Masses crowd in few bins: every lane counts in a column of its own, so that the lanes of a warp never meet.  What bounds it is
+//       the number of instructions per token: 32 sequences x 40 heads of 8192 ... 32768 tokens: 345 us with a shared column per bin
+//       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, see below for now.
 //   evict_move_kernel    a warp per 16 tokens that stay: a lane takes one (tensor, group) of them, a byte load per token (the
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
 //       In place a CTA goes through its (sequence, head) in order: positions only ever move down, and all reads of a turn are done
@@ -17,25 +20,28 @@ namespace cq {
 namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
-constexpr int kBins = 2048;
+constexpr int kBins = 256;
 
-// Whole number of the same order as the mass: any NaN above all numbers, the two zeros alike.
+// Whole number of the same order as the mass, never zero: any NaN above all numbers (a sum with a NaN is the canonical one, which is
+// positive), the two zeros alike.
 __device__ __forceinline__ uint32_t mass_key(float m)
 {
-    if (m != m) return 0xffffffffu;
-    const uint32_t u = __float_as_uint(m + 0.f);
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    const uint32_t u = __float_as_uint(__fadd_rn(m, 0.f));
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// kEach: masses a thread keeps in registers (0: they are read again from memory at every pass)
+constexpr int kFewMost = 1024;                       // tokens that are ranked against each other
+
+// kEach: masses a thread keeps in registers (0: they are read again from memory for every pass)
 template <int kEach>
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ uint32_t hist[kBins];
-    __shared__ uint32_t warp_sum[kSelectWarps];
-    __shared__ uint32_t found[2];                    // bin of the n-th largest, tokens above it
+    __shared__ uint32_t hist[kBins][32];             // later: the keys that are ranked
+    __shared__ uint32_t count[kBins];
+    __shared__ uint32_t found[3];                    // the digit of the last one that stays, tokens above it, tokens with it
+    __shared__ uint32_t few;
     __shared__ uint32_t warp_above[kSelectWarps], warp_equal[kSelectWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int s = blockIdx.x / a.sh.n_kv_heads;
@@ -48,100 +54,137 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictArgs 
         return;
     }
     const int c_lo = a.n_sinks, c_hi = n - a.n_recent;                        // the tokens that compete
+    for (int j = threadIdx.x; j < a.n_sinks; j += kSelectThreads) kept[j] = j;
+    for (int j = threadIdx.x; j < a.n_recent; j += kSelectThreads) kept[a.n_keep - a.n_recent + j] = c_hi + j;
+    kept += a.n_sinks;
     uint32_t need = (uint32_t)(a.n_keep - a.n_sinks - a.n_recent);            // how many of them stay (fewer than there are)
-    // warp w holds per_warp tokens from w * per_warp, register (or turn) j of lane l token j * 32 + l of them
-    const int turns = kEach ? kEach : (n + kSelectThreads - 1) / kSelectThreads;
-    const int base = warp * turns * 32 + lane;
+    if (need == 0u) return;
+    // warp w goes through the tokens from c_lo + w * turns * 32 on, turn j of lane l takes token j * 32 + l of them
+    const int turns = (c_hi - c_lo + kSelectThreads - 1) / kSelectThreads;
+    const int base = c_lo + warp * turns * 32 + lane;
+    auto load = [&](int j) {                                                  // 0: no token (no mass has that key)
+        const int t = base + 32 * j;
+        return j < turns && t < c_hi ? mass_key(mass[t]) : 0u;
+    };
     uint32_t key[kEach ? kEach : 1];
     if (kEach) {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) key[j] = base + 32 * j < n ? mass_key(mass[base + 32 * j]) : 0u;
+        for (int j = 0; j < kEach; ++j) key[j] = load(j);
     }
-    auto key_at = [&](int j) { return kEach ? key[kEach ? j : 0] : (base + 32 * j < n ? mass_key(mass[base + 32 * j]) : 0u); };
-    uint32_t prefix = 0u, mask = 0u;
-    if (need > 0) {
+    auto each = [&](auto&& use) {                                             // use(turn, key) for the warp's tokens, in order
+        if (kEach) {
 #pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : kBins;
-            for (int i = threadIdx.x; i < kBins; i += kSelectThreads) hist[i] = 0u;
-            __syncthreads();
-            auto count = [&](int j) {
-                const int t = base + 32 * j;
-                const uint32_t k = key_at(j);
-                if (t >= c_lo && t < c_hi && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-            };
-            if (kEach) {
+            for (int j = 0; j < kEach; ++j)
+                if (j < turns) use(j, key[kEach ? j : 0]);
+        } else {
+            for (int j = 0; j < turns; ++j) use(j, load(j));
+        }
+    };
+    // Keys above `least` stay, and of those that equal it the first `need`; or (all) every key from `least` on.
+    bool all = false;
+    uint32_t least = 0u, mask = 0u;
+    auto digit = [&](int shift) {                                             // finds the next eight bits
+        for (int i = threadIdx.x; i < kBins * 32; i += kSelectThreads) (&hist[0][0])[i] = 0u;
+        __syncthreads();
+        each([&](int, uint32_t k) {
+            if (k != 0u && (k & mask) == least) atomicAdd(&hist[(k >> shift) & (kBins - 1)][lane], 1u);
+        });
+        __syncthreads();
+        for (int bin = warp; bin < kBins; bin += kSelectWarps) {
+            const uint32_t sum = __reduce_add_sync(0xffffffffu, hist[bin][lane]);
+            if (lane == 0) count[bin] = sum;
+        }
+        __syncthreads();
+        if (warp == 0) {                                                      // lane l: bins 8 l ... 8 l + 7, counted from the top
+            uint32_t c[8], mine = 0u;
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) count(j);
-            } else {
-                for (int j = 0; j < turns; ++j) count(j);
-            }
-            __syncthreads();
-            // thread i owns bins 2 i and 2 i + 1, counted from the top
-            const int top = kBins - 1 - 2 * (int)threadIdx.x;
-            const uint32_t h0 = hist[top], h1 = hist[top - 1];
-            uint32_t incl = h0 + h1;
+            for (int i = 0; i < 8; ++i) { c[i] = count[kBins - 1 - (8 * lane + i)]; mine += c[i]; }
+            uint32_t before = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
+                const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += x;
             }
-            if (lane == 31) warp_sum[warp] = incl;
-            __syncthreads();
-            uint32_t before = 0u;
-            for (int w = 0; w < warp; ++w) before += warp_sum[w];
-            before += incl - h0 - h1;
-            if (before < need && need <= before + h0) { found[0] = (uint32_t)top; found[1] = before; }
-            else if (before + h0 < need && need <= before + h0 + h1) { found[0] = (uint32_t)top - 1u; found[1] = before + h0; }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= (uint32_t)(bins - 1) << shift;
-            need -= found[1];
-            __syncthreads();
-        }
-    }
-    // the keys above `prefix` stay, and the first `need` that equal it (need 0 and prefix 0 with nothing to choose: none)
-    const bool choose = a.n_keep > a.n_sinks + a.n_recent;
-    auto rank = [&](int j, bool& above, bool& equal) {
-        const int t = base + 32 * j;
-        const uint32_t k = key_at(j);
-        const bool forced = t < c_lo || (t >= c_hi && t < n);
-        above = forced || (choose && t < c_hi && k > prefix);
-        equal = choose && !forced && t < c_hi && k == prefix;
-    };
-    uint32_t n_above = 0u, n_equal = 0u;
-    auto tally = [&](int j) {
-        bool above, equal;
-        rank(j, above, equal);
-        n_above += __popc(__ballot_sync(0xffffffffu, above));
-        n_equal += __popc(__ballot_sync(0xffffffffu, equal));
-    };
-    if (kEach) {
+            before -= mine;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) tally(j);
-    } else {
-        for (int j = 0; j < turns; ++j) tally(j);
+            for (int i = 0; i < 8; ++i) {
+                if (before < need && need <= before + c[i]) {
+                    found[0] = (uint32_t)(kBins - 1 - (8 * lane + i));
+                    found[1] = before;
+                    found[2] = c[i];
+                }
+                before += c[i];
+            }
+        }
+        __syncthreads();
+        least |= found[0] << shift;
+        mask |= 0xffu << shift;
+        need -= found[1];
+        all = need == found[2];                                               // the digits so far tell those that stay from the others
+        __syncthreads();
+    };
+    digit(24);
+    if (!all) digit(16);
+    if (!all && found[2] > kFewMost) digit(8);
+    if (!all && found[2] > kFewMost) digit(0);
+    if (!all && mask != 0xffffffffu) {
+        // few share the digits: each is ranked against the others
+        uint32_t* keys = &hist[0][0];
+        if (threadIdx.x == 0) few = 0u;
+        __syncthreads();
+        each([&](int, uint32_t k) {
+            if ((k & mask) == least) keys[atomicAdd(&few, 1u)] = k;           // (not 0: `least` has its highest digits)
+        });
+        __syncthreads();
+        const uint32_t total = few;
+        if (threadIdx.x < total) {
+            const uint32_t k = keys[threadIdx.x];
+            uint32_t above = 0u, equal = 0u;
+            for (uint32_t i = 0; i < total; ++i) {
+                const uint32_t other = keys[i];
+                above += other > k;
+                equal += other == k;
+            }
+            if (above < need && need <= above + equal) {                      // (all that write here hold the same key)
+                found[0] = k;
+                found[1] = above;
+                found[2] = equal;
+            }
+        }
+        __syncthreads();
+        least = found[0];
+        need -= found[1];
+        all = need == found[2];
     }
+    if (all) --least;                                                         // those from `least` on are those above the number before it
+    uint32_t n_above = 0u, n_equal = 0u;
+    each([&](int, uint32_t k) {
+        n_above += k > least;
+        if (!all) n_equal += k == least;
+    });
+    n_above = __reduce_add_sync(0xffffffffu, n_above);
+    n_equal = __reduce_add_sync(0xffffffffu, n_equal);
     if (lane == 0) { warp_above[warp] = n_above; warp_equal[warp] = n_equal; }
     __syncthreads();
-    uint32_t above_before = 0u, equal_before = 0u;
-    for (int w = 0; w < warp; ++w) { above_before += warp_above[w]; equal_before += warp_equal[w]; }
+    uint32_t above_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_above[lane] : 0u);
+    uint32_t equal_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_equal[lane] : 0u);
     const uint32_t below = (1u << lane) - 1u;
-    auto list = [&](int j) {
-        bool above, equal;
-        rank(j, above, equal);
-        const uint32_t eq = __ballot_sync(0xffffffffu, equal), ab = __ballot_sync(0xffffffffu, above);
-        const uint32_t e = equal_before + __popc(eq & below);
-        const uint32_t at = above_before + __popc(ab & below) + (e < need ? e : need);
-        if (above || (equal && e < need)) kept[at] = base + 32 * j;
-        above_before += __popc(ab);
-        equal_before += __popc(eq);
-    };
-    if (kEach) {
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) list(j);
+    if (all) {
+        each([&](int j, uint32_t k) {
+            const bool above = k > least;
+            const uint32_t ab = __ballot_sync(0xffffffffu, above);
+            if (above) kept[above_before + __popc(ab & below)] = base + 32 * j;
+            above_before += __popc(ab);
+        });
     } else {
-        for (int j = 0; j < turns; ++j) list(j);
+        each([&](int j, uint32_t k) {
+            const bool above = k > least, equal = k == least;
+            const uint32_t eq = __ballot_sync(0xffffffffu, equal), ab = __ballot_sync(0xffffffffu, above);
+            const uint32_t e = equal_before + __popc(eq & below);
+            if (above || (equal && e < need)) kept[above_before + __popc(ab & below) + (e < need ? e : need)] = base + 32 * j;
+            above_before += __popc(ab);
+            equal_before += __popc(eq);
+        });
     }
 }
 

@@ -191,7 +191,9 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictArgs 
 constexpr int kMoveWarps = 8;
 
 // One CTA: out blocks blockIdx.y * per_cta ... of (sequence, head) blockIdx.x; in place one CTA takes them all.
-__global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a, int per_cta, int in_place)
+// kHigh: codes wider than a byte; kInPlace.
+template <bool kHigh, bool kInPlace>
+__global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a, int per_cta)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Shape& sh = a.sh;
@@ -212,20 +214,34 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a
     for (int b0 = first; b0 < last; b0 += kMoveWarps) {
         const int ob = b0 + warp;
         const int j = ob * kTokenBlock + (lane & 15);
-        const int idx = ob < last && j < left ? kept[j] : -1;                 // lane k and k + 16: source of token k
-        const float m = idx >= 0 ? mass[idx] : 0.f;
+        const bool there = ob < last && j < left;
+        const int idx = there ? kept[j] : 0;                                  // lanes k and k + 16: the source of token k (none: any)
+        const int64_t at = (int64_t)(idx / kTokenBlock) * sh.block_bytes + idx % kTokenBlock;
+        const uint32_t none = __ballot_sync(0xffffffffu, !there) & 0xffffu;
+        const float m = there ? mass[idx] : 0.f;
         for (int w0 = 0; w0 < words; w0 += 32) {
             const int w = w0 + lane, tensor = w >= sh.G, g = tensor ? w - sh.G : w;
             const bool live = ob < last && w < words;
-            const uint8_t* src = (tensor ? a.vc : a.kc) + from;
+            const uint8_t* src = (tensor ? a.vc : a.kc) + from + (live ? g * kTokenBlock : 0);
             uint32_t lo[4] = {0u, 0u, 0u, 0u}, hi[4] = {0u, 0u, 0u, 0u};
+            if (ob < last) {
+                uint32_t byte[kTokenBlock];
 #pragma unroll
-            for (int k = 0; k < kTokenBlock; ++k) {
-                const int t = __shfl_sync(0xffffffffu, idx, k);
-                if (live && t >= 0) {
-                    const uint8_t* blk = src + (int64_t)(t / kTokenBlock) * sh.block_bytes;
-                    lo[k >> 2] |= (uint32_t)blk[g * kTokenBlock + t % kTokenBlock] << (8 * (k & 3));
-                    if (sh.hb) {
+                for (int k = 0; k < kTokenBlock; ++k) byte[k] = src[__shfl_sync(0xffffffffu, at, k)];
+#pragma unroll
+                for (int k = 0; k < kTokenBlock; k += 4)
+                    lo[k >> 2] = __byte_perm(__byte_perm(byte[k], byte[k + 1], 0x0040), __byte_perm(byte[k + 2], byte[k + 3], 0x0040), 0x5410);
+                if (none) {                                                   // behind the last token: zeros
+#pragma unroll
+                    for (int k = 0; k < kTokenBlock; ++k)
+                        if ((none >> k) & 1u) lo[k >> 2] &= ~(0xffu << (8 * (k & 3)));
+                }
+                if (kHigh) {
+#pragma unroll
+                    for (int k = 0; k < kTokenBlock; ++k) {
+                        const int t = __shfl_sync(0xffffffffu, idx, k);
+                        if (!live || ((none >> k) & 1u)) continue;
+                        const uint8_t* blk = (tensor ? a.vc : a.kc) + from + (int64_t)(t / kTokenBlock) * sh.block_bytes;
                         const uint32_t high = (uint32_t)read_code(blk, sh, g, t % kTokenBlock) >> 8;
                         const int bit = k * sh.hb;
 #pragma unroll
@@ -234,10 +250,10 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a
                     }
                 }
             }
-            if (in_place) __syncthreads();
+            if (kInPlace) __syncthreads();
             if (live) {
                 uint8_t* dst = (tensor ? a.v_out : a.k_out) + to + (int64_t)ob * sh.block_bytes;
-                if (sh.hb == 0) {
+                if (!kHigh) {
                     *reinterpret_cast<uint4*>(dst + g * kTokenBlock) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 } else {                                                      // blocks of wide codes start at even bytes
 #pragma unroll
@@ -249,7 +265,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a
                 }
             }
         }
-        if (lane < kTokenBlock && idx >= 0) mass_out[j] = m;
+        if (lane < kTokenBlock && there) mass_out[j] = m;
     }
 }
 
@@ -266,7 +282,7 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
     else if (a.sh.max_tokens <= 32 * kSelectThreads) e = cudaLaunchKernelEx(&cfg, evict_select_kernel<32>, a);
     else e = cudaLaunchKernelEx(&cfg, evict_select_kernel<0>, a);
     if (e != cudaSuccess) return e;
-    const int in_place = a.k_out == a.kc;
+    const bool in_place = a.k_out == a.kc;
     const int64_t most = a.n_keep < a.sh.max_tokens ? a.n_keep : a.sh.max_tokens;
     const int n_out = (int)((most + kTokenBlock - 1) / kTokenBlock);
     int per_cta = in_place ? n_out : 4 * kMoveWarps;
@@ -274,7 +290,8 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
     cudaLaunchAttribute attr2;
     cudaLaunchConfig_t move = overlapped_config((unsigned)items, kMoveWarps * 32, 0, st, &attr2);
     move.gridDim = dim3((unsigned)items, (unsigned)((n_out + per_cta - 1) / per_cta));
-    return cudaLaunchKernelEx(&move, evict_move_kernel, a, per_cta, in_place);
+    if (a.sh.hb) return in_place ? cudaLaunchKernelEx(&move, evict_move_kernel<true, true>, a, per_cta) : cudaLaunchKernelEx(&move, evict_move_kernel<true, false>, a, per_cta);
+    return in_place ? cudaLaunchKernelEx(&move, evict_move_kernel<false, true>, a, per_cta) : cudaLaunchKernelEx(&move, evict_move_kernel<false, false>, a, per_cta);
 }
 
 }  // namespace cq

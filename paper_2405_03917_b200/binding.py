@@ -572,6 +572,12 @@ def cq_window_attn(q: torch.Tensor, k_codes: torch.Tensor, v_codes: torch.Tensor
     """Attention of the n_q newest cached tokens with a sliding window (0: none) and the n_sinks first tokens visible.
     q fp16 (n_seq, n_q, Hq, head_dim); codebooks fp16 (Hkv, G, 2^b, c); seq_lens int32 (n_seq,) counts the new tokens.
     Returns out fp16 like q."""
+    st = (_native_module or _native()).window_attn(q, k_codes, v_codes, k_cb, v_cb, seq_lens, scale, c, b, max_tokens, window, n_sinks, out, workspace,
+                                                   variant)
+    if st is not None:
+        if st:
+            raise CQError(st, "cq_window_attn")
+        return out
     n_seq, n_q, n_q_heads, head_dim = q.shape
     n_kv_heads = k_cb.shape[0]
     _hold(cq_codes_bytes(n_seq, max_tokens, n_kv_heads, head_dim, c, b), k_codes=k_codes, v_codes=v_codes)
@@ -607,6 +613,12 @@ def cq_paged_attn(q: torch.Tensor, q_offsets: torch.Tensor, k_pages: torch.Tenso
     sequence s (int32, n_seq + 1 entries, at most max_q per sequence); k_pages / v_pages uint8 pools of pages of page_tokens tokens;
     page_table int32 (n_seq, pages_per_seq); seq_lens counts the new tokens.  Returns out fp16 like q; rows of no sequence are left
     as they were."""
+    st = (_native_module or _native()).paged_attn(q, q_offsets, k_pages, v_pages, k_cb, v_cb, page_table, seq_lens, scale, c, b, page_tokens, max_q, window,
+                                                  n_sinks, out, workspace, variant)
+    if st is not None:
+        if st:
+            raise CQError(st, "cq_paged_attn")
+        return out
     n_rows, n_q_heads, head_dim = q.shape
     n_kv_heads = k_cb.shape[0]
     n_seq, pages_per_seq = page_table.shape
@@ -667,6 +679,11 @@ def cq_attn_mass(q: torch.Tensor, k_codes: torch.Tensor, k_cb: torch.Tensor, seq
     """Adds the attention weight that every cached token receives from the n_q newest tokens: q fp16 (n_seq, n_q, Hq, head_dim),
     mass fp32 (n_seq, Hkv, max_tokens) or None (zeros).  Returns mass_out, which may be mass; a mass_out that the call makes is
     zero behind the lengths."""
+    st = (_native_module or _native()).attn_mass(q, k_codes, k_cb, seq_lens, scale, c, b, max_tokens, mass, mass_out, workspace, variant)
+    if st is not None:
+        if st:
+            raise CQError(st, "cq_attn_mass")
+        return mass_out
     n_seq, n_q, n_q_heads, head_dim = q.shape
     n_kv_heads = k_cb.shape[0]
     shape = (n_seq, n_kv_heads, max_tokens)
@@ -698,6 +715,15 @@ def cq_evict(mass: torch.Tensor, k_codes: torch.Tensor, v_codes: torch.Tensor, s
     if not any(given):
         k_codes_out, v_codes_out, mass_out = k_codes, v_codes, mass
     room = max_tokens if out_max_tokens is None else out_max_tokens
+    if mass.is_cuda:
+        kept = torch.empty(n_seq, n_heads, n_keep, dtype=torch.int32, device=mass.device) if kept is None and n_keep > 0 else kept
+        seq_lens_out = torch.empty(n_seq, dtype=torch.int32, device=mass.device) if seq_lens_out is None else seq_lens_out
+    st = (_native_module or _native()).evict(mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, room, mass_out,
+                                             k_codes_out, v_codes_out, kept, seq_lens_out)
+    if st is not None:
+        if st:
+            raise CQError(st, "cq_evict")
+        return kept, seq_lens_out
     _hold(cq_codes_bytes(n_seq, max_tokens, n_heads, head_dim, c, b), k_codes=k_codes, v_codes=v_codes)
     _hold(cq_codes_bytes(n_seq, room, n_heads, head_dim, c, b), k_codes_out=k_codes_out, v_codes_out=v_codes_out)
     with _one_device(mass, k_codes, v_codes, seq_lens, k_codes_out, v_codes_out, mass_out, kept, seq_lens_out):

@@ -8,8 +8,11 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
 
 #include "../../include/cq.h"
 
@@ -226,6 +229,103 @@ PyObject* encode_kv(PyObject*, PyObject* const* argv, Py_ssize_t n)
                 vc->data_ptr(), current_stream());
 }
 
+// The operators on bounded caches run on the device of their tensors: the native call covers the usual case, that it is the current one.
+bool on_current_device(std::initializer_list<const at::Tensor*> tensors)
+{
+    const c10::DeviceIndex dev = c10::cuda::current_device();
+    for (const at::Tensor* t : tensors)
+        if (t && t->device().index() != dev) return false;
+    return true;
+}
+
+// q, k_codes, v_codes, k_cb, v_cb, seq_lens, scale, c, b, max_tokens, window, n_sinks, out, workspace, variant
+PyObject* window_attn(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    if (n != 15) Py_RETURN_NONE;
+    Args a{argv};
+    const at::Tensor *q = a.device(0, kHalf), *kc = a.device(1, kByte), *vc = a.device(2, kByte), *kb = a.device(3, kHalf), *vb = a.device(4, kHalf);
+    const at::Tensor* sl = a.device(5, kInt);
+    const float scale = a.real(6);
+    const int c = a.small(7), b = a.small(8);
+    const int64_t cap = a.integer(9), window = a.integer(10), sinks = a.integer(11);
+    const at::Tensor *out = a.device(12, kHalf), *ws = a.device(13, kByte);
+    const int variant = a.small(14);
+    if (!a.ok || q->dim() != 4 || kb->dim() != 4 || !on_current_device({q, kc, vc, kb, vb, sl, out, ws})) Py_RETURN_NONE;
+    const int64_t ns = q->size(0), nq = q->size(1), hq = q->size(2), D = q->size(3), hkv = kb->size(0);
+    if (nq > INT_MAX || !is_book(*kb, hkv, D, c, b) || !is_book(*vb, hkv, D, c, b) || sl->numel() != ns || out->sizes() != q->sizes() ||
+        !hold_codes(*kc, *vc, ns, cap, hkv, D, c, b))
+        Py_RETURN_NONE;
+    return call(cq_window_attn_variant, q->data_ptr(), kc->data_ptr(), vc->data_ptr(), kb->data_ptr(), vb->data_ptr(), (const int32_t*)sl->data_ptr(),
+                scale, window, sinks, (int)ns, (int)nq, (int)hq, (int)hkv, (int)D, c, b, cap, out->data_ptr(), ws->data_ptr(), (size_t)ws->numel(),
+                variant, current_stream());
+}
+
+// q, q_offsets, k_pages, v_pages, k_cb, v_cb, page_table, seq_lens, scale, c, b, page_tokens, max_q, window, n_sinks, out, workspace, variant
+PyObject* paged_attn(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    if (n != 18) Py_RETURN_NONE;
+    Args a{argv};
+    const at::Tensor *q = a.device(0, kHalf), *qo = a.device(1, kInt), *kp = a.device(2, kByte), *vp = a.device(3, kByte), *kb = a.device(4, kHalf);
+    const at::Tensor *vb = a.device(5, kHalf), *pt = a.device(6, kInt), *sl = a.device(7, kInt);
+    const float scale = a.real(8);
+    const int c = a.small(9), b = a.small(10);
+    const int64_t page = a.integer(11);
+    const int max_q = a.small(12);
+    const int64_t window = a.integer(13), sinks = a.integer(14);
+    const at::Tensor *out = a.device(15, kHalf), *ws = a.device(16, kByte);
+    const int variant = a.small(17);
+    if (!a.ok || q->dim() != 3 || kb->dim() != 4 || pt->dim() != 2 || !on_current_device({q, qo, kp, vp, kb, vb, pt, sl, out, ws})) Py_RETURN_NONE;
+    const int64_t rows = q->size(0), hq = q->size(1), D = q->size(2), hkv = kb->size(0), ns = pt->size(0), per_seq = pt->size(1);
+    const int64_t page_bytes = (int64_t)cq_codes_bytes(16, page, (int)hkv, (int)D, c, b) / 16;
+    if (rows == 0 || page_bytes == 0 || !is_book(*kb, hkv, D, c, b) || !is_book(*vb, hkv, D, c, b) || qo->numel() != ns + 1 || sl->numel() != ns ||
+        out->sizes() != q->sizes())
+        Py_RETURN_NONE;
+    return call(cq_paged_attn_variant, q->data_ptr(), (const int32_t*)qo->data_ptr(), kp->data_ptr(), vp->data_ptr(), kb->data_ptr(), vb->data_ptr(),
+                (const int32_t*)pt->data_ptr(), (const int32_t*)sl->data_ptr(), scale, window, sinks, (int)ns, rows, max_q, (int)hq, (int)hkv, (int)D, c,
+                b, std::min(kp->numel(), vp->numel()) / page_bytes, page, per_seq, out->data_ptr(), ws->data_ptr(), (size_t)ws->numel(), variant,
+                current_stream());
+}
+
+// q, k_codes, k_cb, seq_lens, scale, c, b, max_tokens, mass | None, mass_out, workspace, variant
+PyObject* attn_mass(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    if (n != 12) Py_RETURN_NONE;
+    Args a{argv};
+    const at::Tensor *q = a.device(0, kHalf), *kc = a.device(1, kByte), *kb = a.device(2, kHalf), *sl = a.device(3, kInt);
+    const float scale = a.real(4);
+    const int c = a.small(5), b = a.small(6);
+    const int64_t cap = a.integer(7);
+    const at::Tensor *in = a.optional(8, kFloat), *out = a.device(9, kFloat), *ws = a.device(10, kByte);
+    const int variant = a.small(11);
+    if (!a.ok || q->dim() != 4 || kb->dim() != 4 || !on_current_device({q, kc, kb, sl, in, out, ws})) Py_RETURN_NONE;
+    const int64_t ns = q->size(0), nq = q->size(1), hq = q->size(2), D = q->size(3), hkv = kb->size(0);
+    if (nq > INT_MAX || !is_book(*kb, hkv, D, c, b) || sl->numel() != ns || !is_shape(*out, {ns, hkv, cap}) || (in && !is_shape(*in, {ns, hkv, cap})) ||
+        !hold_codes(*kc, *kc, ns, cap, hkv, D, c, b))
+        Py_RETURN_NONE;
+    return call(cq_attn_mass_variant, q->data_ptr(), kc->data_ptr(), kb->data_ptr(), (const int32_t*)sl->data_ptr(), scale,
+                in ? (const float*)in->data_ptr() : nullptr, (int)ns, (int)nq, (int)hq, (int)hkv, (int)D, c, b, cap, (float*)out->data_ptr(),
+                ws->data_ptr(), (size_t)ws->numel(), variant, current_stream());
+}
+
+// mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, out_max_tokens, mass_out, k_out, v_out, kept, lens_out
+PyObject* evict(PyObject*, PyObject* const* argv, Py_ssize_t n)
+{
+    if (n != 17) Py_RETURN_NONE;
+    Args a{argv};
+    const at::Tensor *m = a.device(0, kFloat), *kc = a.device(1, kByte), *vc = a.device(2, kByte), *sl = a.device(3, kInt);
+    const int D = a.small(4), c = a.small(5), b = a.small(6);
+    const int64_t cap = a.integer(7), keep = a.integer(8), sinks = a.integer(9), recent = a.integer(10), room = a.integer(11);
+    const at::Tensor *mo = a.device(12, kFloat), *ko = a.device(13, kByte), *vo = a.device(14, kByte), *kept = a.device(15, kInt), *lo = a.device(16, kInt);
+    if (!a.ok || m->dim() != 3 || !on_current_device({m, kc, vc, sl, mo, ko, vo, kept, lo})) Py_RETURN_NONE;
+    const int64_t ns = m->size(0), h = m->size(1);
+    if (!is_shape(*m, {ns, h, cap}) || !is_shape(*mo, {ns, h, room}) || sl->numel() != ns || !is_shape(*kept, {ns, h, keep}) || !is_shape(*lo, {ns}) ||
+        !hold_codes(*kc, *vc, ns, cap, h, D, c, b) || !hold_codes(*ko, *vo, ns, room, h, D, c, b))
+        Py_RETURN_NONE;
+    return call(cq_evict, (const float*)m->data_ptr(), kc->data_ptr(), vc->data_ptr(), (const int32_t*)sl->data_ptr(), (int)ns, (int)h, D, c, b, cap, keep,
+                sinks, recent, room, (float*)mo->data_ptr(), ko->data_ptr(), vo->data_ptr(), (int32_t*)kept->data_ptr(), (int32_t*)lo->data_ptr(),
+                current_stream());
+}
+
 // torch throws where a tensor has no memory (under tracing or vmap) or no current stream: no exception may leave for the
 // interpreter.  Nothing has been called then, and the wrapper's own checks meet the same error as a Python exception.
 template <PyObject* (*function)(PyObject*, PyObject* const*, Py_ssize_t)>
@@ -240,7 +340,8 @@ PyObject* guarded(PyObject* self, PyObject* const* argv, Py_ssize_t n)
 
 #define CQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<&name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CQ_METHOD(decode_step), CQ_METHOD(decode_step_host), CQ_METHOD(decode_attn), CQ_METHOD(decode_attn_rope),
-                         CQ_METHOD(prefill_attn), CQ_METHOD(encode), CQ_METHOD(encode_kv), {nullptr, nullptr, 0, nullptr}};
+                         CQ_METHOD(prefill_attn), CQ_METHOD(encode), CQ_METHOD(encode_kv), CQ_METHOD(window_attn), CQ_METHOD(paged_attn), CQ_METHOD(attn_mass),
+                         CQ_METHOD(evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cq_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -518,7 +518,9 @@ int cq_paged_append(const void *k_fp16, const void *v_fp16, const int32_t *q_off
  *
  *   mass_in      NULL (zeros), or fp32 [n_seq][n_kv_heads][max_tokens], device
  *   mass_out     the same shape, may be mass_in; positions from seq_lens[s] on are left as they were
- *   workspace    at least cq_attn_mass_workspace_bytes(...) bytes, 16-byte aligned
+ *   workspace    cq_attn_mass_workspace_bytes(...) bytes, 16-byte aligned.  For up to four rows (query tokens x query heads of a
+ *                KV head) they hold the scores between the two passes, 16 bytes per cached token and KV head.  What the same call
+ *                with max_tokens = n_q_tokens asks for is enough: the second pass then works the scores out again
  * Sums are formed in a fixed order: two calls on the same inputs give the same bits.
  * variant: 0 = automatic, 1 = plain kernels, 2 = tensor-core kernel (head_dim 128, one byte per code, c = 2, 4 or 8).
  */

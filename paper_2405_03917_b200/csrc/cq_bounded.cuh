@@ -103,7 +103,8 @@ size_t gather_attn_workspace_bytes();
 cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
 // the masses with the same scores (uniform rows, a contiguous cache, no window); the same shapes
 size_t gather_mass_workspace_bytes(const BoundedArgs& a);
-cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st);
+size_t gather_mass_least_bytes(const BoundedArgs& a);      // what it cannot do without
+cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, size_t workspace_bytes, cudaStream_t st);
 
 // many rows per sequence (cq_chunk_attn.cu): the tensor-core kernel of the prefill attention in its bounded form
 bool chunk_attn_supported(const Shape& sh);

@@ -203,12 +203,18 @@ int cq_paged_append(const void* k_fp16, const void* v_fp16, const int32_t* q_off
                                         static_cast<cudaStream_t>(stream)));
 }
 
+static size_t mass_workspace(const BoundedArgs& a, bool least)
+{
+    const size_t plain = round_up((size_t)a.n_rows * a.sh.n_q_heads * sizeof(float), 256);
+    const size_t tuned = !gather_attn_supported(a.sh) ? 0 : least ? gather_mass_least_bytes(a) : gather_mass_workspace_bytes(a);
+    return plain > tuned ? plain : tuned;
+}
+
 size_t cq_attn_mass_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b, int64_t max_tokens)
 {
     BoundedArgs a;
     if (bounded_shape(n_seq, (int64_t)n_seq * n_q_tokens, n_q_tokens, max_tokens, n_q_heads, n_kv_heads, head_dim, c, b, 0, 0, &a) != CQ_OK) return 0;
-    const size_t plain = round_up((size_t)a.n_rows * n_q_heads * sizeof(float), 256), tuned = gather_attn_supported(a.sh) ? gather_mass_workspace_bytes(a) : 0;
-    return plain > tuned ? plain : tuned;
+    return mass_workspace(a, false);
 }
 
 int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_cb_fp16, const int32_t* seq_lens, float scale,
@@ -222,7 +228,7 @@ int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_
     if (!aligned16(q_fp16) || !aligned16(k_codes) || !aligned16(k_cb_fp16) || !aligned16(workspace) || !aligned4(seq_lens) || !aligned4(mass_in) ||
         !aligned4(mass_out))
         return CQ_ERR_ALIGN;
-    if (workspace_bytes < cq_attn_mass_workspace_bytes(n_seq, n_q_tokens, n_q_heads, n_kv_heads, head_dim, c, b, max_tokens)) return CQ_ERR_WORKSPACE;
+    if (workspace_bytes < mass_workspace(a, true)) return CQ_ERR_WORKSPACE;
     if (variant < 0 || variant > 2) return CQ_ERR_SHAPE;
     if (variant == 2 && !gather_attn_supported(a.sh)) return CQ_ERR_UNSUPPORTED;
     a.q = static_cast<const __half*>(q_fp16);
@@ -230,7 +236,7 @@ int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_
     a.kcb = static_cast<const __half*>(k_cb_fp16);
     a.seq_lens = seq_lens;
     a.scale_log2e = scale * kLog2e;
-    if (variant != 1 && gather_attn_supported(a.sh)) return status(launch_gather_mass(a, mass_in, mass_out, workspace, static_cast<cudaStream_t>(stream)));
+    if (variant != 1 && gather_attn_supported(a.sh)) return status(launch_gather_mass(a, mass_in, mass_out, workspace, workspace_bytes, static_cast<cudaStream_t>(stream)));
     return status(launch_mass_plain(a, mass_in, mass_out, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }
 

@@ -21,9 +21,11 @@
 // takes about 115 cycles, 80 of them wavefronts.  64 sequences, 32 heads on 8, CQ-8c8b: window of 4096 81 us, contexts of
 // 4096 ... 16384 in pages 166 us = 1.0 TB/s.
 //
-// Masses take two passes over the key codes with the same scores: kLse leaves every row's log-sum-exp, kMass turns scores into
-// weights and adds up, per token, those of all rows.  (Row after row tile goes over the same blocks in the same CTA: every sum has one
-// writer and one order.)  They need the key centroids only, so two CTAs share an SM.
+// Masses take two passes: kLse leaves every row's log-sum-exp and, for up to four rows, the scores; mass_of_scores_kernel turns these into
+// weights and adds up, per token, those of all rows.  Where scores are not kept, kMass works them out again.  (Row after row tile goes
+// over the same blocks in the same CTA: every sum has one writer and one order.)  Keys alone leave room for two CTAs on an SM (one:
+// 450 against 291 us; ten or twelve warps instead of eight spill: 175 and 179 against 160 us).  64 sequences of 16384 tokens, 32 heads
+// on 8, CQ-8c8b: 291 us without stored scores, 160 us with them.
 //
 // Work is dealt evenly: the blocks that all (KV head, sequence, row tile) items attend lie on one line, every CTA takes an equal
 // stretch of it (a stretch that crosses into another KV head loads that head's centroids), and what a cut item leaves behind
@@ -42,11 +44,11 @@ enum Mode { kAttn, kLse, kMass };
 constexpr int kBookBytes = 256 * 256;
 // Eight warps (12 were as fast: 81 and 82 us for 64 sequences with a window of 4096, 32 heads on 8), and their share of the rest of
 // shared memory: codes on their way (2 blocks' for c = 2, 4 for c = 4, 8 for c = 8), then accumulators.
-constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kKOffset = 0, kVOffset = kBookBytes;
 template <int kMode>
 struct Cfg {
     static constexpr int kCtas = kMode == kAttn ? 1 : 2;                      // of an SM
+    static constexpr int kWarps = 8, kThreads = kWarps * 32;
     static constexpr int kWarpBytes = kMode == kAttn ? 4096 : 2048;
     static constexpr int kStageOffset = kMode == kAttn ? 3 * kBookBytes : kBookBytes;
     static constexpr int kStatOffset = kStageOffset + kWarps * kWarpBytes;    // [warp][8] references, [warp][8] sums, what the scans need
@@ -64,6 +66,7 @@ struct MassArgs {
     float* mass_out;
     float* lse;                                                           // [sequence][KV head][row_stride]: log2 of the sum of 2^score
     int row_stride;
+    float* scores;                                                        // null, or the scores (log2 domain) of four rows: [sequence][KV head][block][row][16]
 };
 
 // What a CTA leaves of the items that its stretch cuts: [0] the end or the middle of one, [1] the beginning of one.
@@ -166,6 +169,7 @@ __device__ __forceinline__ void place_of(int reg, int lane, int& row, int& chann
 }
 
 // Sum of `v` over the threads before this one, and over all; every thread takes part.
+template <int kWarps>
 __device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t* scratch, int64_t& total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -188,11 +192,11 @@ __device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t* scratch, int
 }
 
 template <int kC, int kRows, int kMode>
-__global__ void __launch_bounds__(kThreads, Cfg<kMode>::kCtas)
+__global__ void __launch_bounds__(Cfg<kMode>::kThreads, Cfg<kMode>::kCtas)
 gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* __restrict__ cuts)
 {
     using C = Cfg<kMode>;
-    constexpr int kWarpBytes = C::kWarpBytes;
+    constexpr int kWarps = C::kWarps, kThreads = C::kThreads, kWarpBytes = C::kWarpBytes;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int G = 128 / kC, E = kC / 2;
@@ -223,7 +227,7 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
     for (int s0 = 0; s0 < n_seq; s0 += kThreads) {
         int64_t all;
         mine = blocks_of(s0 + (int)threadIdx.x);
-        before = block_prefix(mine, scratch, all);
+        before = block_prefix<kWarps>(mine, scratch, all);
         per_head += all;
     }
     const int64_t total = per_head * sh.n_kv_heads;
@@ -239,7 +243,7 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
         int64_t all = per_head;
         if (n_seq > kThreads) {                                             // (otherwise the first scan's results are still there)
             mine = blocks_of(s0 + (int)threadIdx.x);
-            before = block_prefix(mine, scratch, all);
+            before = block_prefix<kWarps>(mine, scratch, all);
         }
         if (rest >= all) { rest -= all; continue; }
         if (before <= rest && rest < before + mine) { scratch[0] = s0 + (int)threadIdx.x; scratch[1] = rest - before; }
@@ -513,6 +517,9 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
                 }
             }
         };
+        float* scores = nullptr;                                            // the lane's place in a block's
+        if (kMode == kLse && kRows == 4 && mass.scores)
+            scores = mass.scores + ((int64_t)it.seq * sh.n_kv_heads + it.head) * sh.n_blocks * 64 + p * 16 + 2 * r;
         if constexpr (kMode == kMass) {
             m_ref = reinterpret_cast<const float*>(smem + C::kQOffset + 2048)[my_row];
             sums = mass.mass_out + ((int64_t)it.seq * sh.n_kv_heads + it.head) * sh.max_tokens;
@@ -630,6 +637,9 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
             if constexpr (kMode == kLse) {
 #pragma unroll
                 for (int j = 0; j < kSc; ++j) l += ex2f(fmaf(sc[j], scale, -ref));
+                const int blk = block_of(it, turn);
+                if (kRows == 4 && scores && blk >= 0)
+                    *reinterpret_cast<float2*>(scores + (int64_t)blk * 64) = make_float2(sc[0] * scale, sc[1] * scale);
             } else {
             uint32_t y[kSc / 2];
 #pragma unroll
@@ -839,6 +849,39 @@ gather_merge_kernel(BoundedArgs a, MassArgs mass, const float* __restrict__ part
     }
 }
 
+constexpr int kStreamThreads = 256, kStreamEach = 4;                        // tokens of a thread
+
+// Masses from stored scores of up to four rows: a thread per token, the rows' weights in the order of the rows.
+__global__ void __launch_bounds__(kStreamThreads) mass_of_scores_kernel(BoundedArgs a, MassArgs mass, int chunks)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t item = blockIdx.x / chunks;                               // (sequence, KV head)
+    const int64_t n64 = a.seq_lens[item / a.sh.n_kv_heads];
+    const int n = (int)(n64 < 0 ? 0 : (n64 > a.sh.max_tokens ? a.sh.max_tokens : n64));
+    const int t0 = (int)(blockIdx.x % chunks) * (kStreamThreads * kStreamEach) + (int)threadIdx.x;
+    if (t0 - (int)threadIdx.x >= n) return;
+    const int rows = a.max_q * a.sh.R;
+    float lse[4], x[kStreamEach][4], was[kStreamEach];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) lse[r] = r < rows ? mass.lse[item * mass.row_stride + r] : 0.f;
+    const float* scores = mass.scores + item * a.sh.n_blocks * 64;
+#pragma unroll
+    for (int u = 0; u < kStreamEach; ++u) {
+        const int t = t0 + u * kStreamThreads;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[u][r] = t < n && r < rows ? scores[(int64_t)(t / kTokenBlock) * 64 + r * 16 + t % kTokenBlock] : -INFINITY;
+        was[u] = t < n && mass.mass_in ? mass.mass_in[item * a.sh.max_tokens + t] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kStreamEach; ++u) {
+        const int t = t0 + u * kStreamThreads;
+        float w = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w += x[u][r] == -INFINITY ? 0.f : ex2f(x[u][r] - lse[r]);
+        if (t < n) mass.mass_out[item * a.sh.max_tokens + t] = was[u] + w;
+    }
+}
+
 template <int kC, int kRows, int kMode>
 cudaError_t launch(const BoundedArgs& a, const MassArgs& mass, void* workspace, int slot, cudaStream_t st)
 {
@@ -849,7 +892,7 @@ cudaError_t launch(const BoundedArgs& a, const MassArgs& mass, void* workspace, 
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(gather_kernel<kC, kRows, kMode>), C::kSmemBytes, slot);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr;
-    cudaLaunchConfig_t cfg = overlapped_config((unsigned)grid, kThreads, C::kSmemBytes, st, &attr);
+    cudaLaunchConfig_t cfg = overlapped_config((unsigned)grid, C::kThreads, C::kSmemBytes, st, &attr);
     e = cudaLaunchKernelEx(&cfg, gather_kernel<kC, kRows, kMode>, a, mass, partials, cuts);
     if (e != cudaSuccess || kMode == kMass) return e;
     cfg.dynamicSmemBytes = 0;
@@ -883,19 +926,32 @@ bool gather_attn_supported(const Shape& sh) { return sh.head_dim == 128 && sh.b 
 size_t gather_attn_workspace_bytes() { return gather_bytes(kAttn); }
 cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st) { return launch_mode<kAttn>(a, MassArgs(), workspace, 100, st); }
 
-size_t gather_mass_workspace_bytes(const BoundedArgs& a)
-{
-    return gather_bytes(kLse) + round_up((size_t)a.sh.n_seq * a.sh.n_kv_heads * mass_row_stride(a) * sizeof(float), 256);
-}
-cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st)
+namespace {
+size_t lse_bytes(const BoundedArgs& a) { return gather_bytes(kLse) + round_up((size_t)a.sh.n_seq * a.sh.n_kv_heads * mass_row_stride(a) * sizeof(float), 256); }
+// Bytes of the scores of one step's rows, where they are few: 16 bytes per cached token and KV head, as many as the key codes of c = 8.
+size_t score_bytes(const BoundedArgs& a) { return a.max_q * a.sh.R <= 4 ? (size_t)a.sh.n_seq * a.sh.n_kv_heads * a.sh.n_blocks * 64 * sizeof(float) : 0; }
+}  // namespace
+
+size_t gather_mass_workspace_bytes(const BoundedArgs& a) { return lse_bytes(a) + score_bytes(a); }
+size_t gather_mass_least_bytes(const BoundedArgs& a) { return lse_bytes(a); }
+// With room for the scores the second pass reads them; otherwise it works them out again.
+cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, size_t workspace_bytes, cudaStream_t st)
 {
     MassArgs mass;
     mass.mass_in = mass_in;
     mass.mass_out = mass_out;
     mass.lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + gather_bytes(kLse));
     mass.row_stride = mass_row_stride(a);
+    const bool store = score_bytes(a) && workspace_bytes >= gather_mass_workspace_bytes(a);
+    mass.scores = store ? reinterpret_cast<float*>(static_cast<char*>(workspace) + lse_bytes(a)) : nullptr;
     const cudaError_t e = launch_mode<kLse>(a, mass, workspace, 109, st);
-    return e != cudaSuccess ? e : launch_mode<kMass>(a, mass, workspace, 115, st);
+    if (e != cudaSuccess) return e;
+    if (!store) return launch_mode<kMass>(a, mass, workspace, 115, st);
+    const int64_t chunks = (a.sh.max_tokens + kStreamThreads * kStreamEach - 1) / (kStreamThreads * kStreamEach), grid = a.sh.n_seq * a.sh.n_kv_heads * chunks;
+    if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = overlapped_config((unsigned)grid, kStreamThreads, 0, st, &attr);
+    return cudaLaunchKernelEx(&cfg, mass_of_scores_kernel, a, mass, (int)chunks);
 }
 
 }  // namespace cq

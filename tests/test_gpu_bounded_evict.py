@@ -206,3 +206,18 @@ def test_evict_in_a_graph_and_on_another_stream():
     assert torch.equal(kept, kept2) and torch.equal(left, left2)
     for name in ("k_codes_out", "v_codes_out", "mass_out"):
         assert torch.equal(a[name], b_[name])
+
+
+def test_mass_with_less_workspace():
+    # without room for the scores the second pass works them out again: the same masses up to the order of a few additions
+    case = B.Case(12, 8, 8, 8, 2, [1500, 33, 700], 1504)
+    q = case.queries(3, 1)
+    k, _ = case.contiguous()
+    full = cq.cq_attn_mass_workspace_bytes(3, 1, 8, 2, 128, 8, 8, 1504)
+    least = cq.cq_attn_mass_workspace_bytes(3, 1, 8, 2, 128, 8, 8, 1)
+    assert least < full
+    call = lambda size: cq.cq_attn_mass(q, k, case.kcb, case.seq_lens(), SCALE, 8, 8, 1504, workspace=torch.empty(size, dtype=torch.uint8, device=DEV))
+    for got in (call(full), call(least)):
+        for s, n in enumerate(case.lens):
+            _, _, p = B.attend(case, s, q[s], n, SCALE)
+            assert ((got[s, :, :n].double() - p.view(2, -1, n).sum(1)).abs() <= mass_tolerance(case, s, q[s], n, p)).all()

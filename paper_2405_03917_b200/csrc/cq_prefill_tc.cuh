@@ -372,8 +372,19 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             }
         }
     }
+    // bounded: whether any page that this CTA may attend is missing (then the softmax warps look for holes, tile by tile)
+    bool missing = false;
+    if constexpr (kBounded) {
+        const BoundedArgs& a = bounded.a;
+        if (a.page_table && pos_last >= 0)
+            for (int i = threadIdx.x; i <= a.page_div.quotient((int)(pos_last / kTokenBlock)); i += C::kThreads) {
+                const int page = a.page_table[s * a.pages_per_seq + i];
+                missing |= page < 0 || page >= a.n_pages;
+            }
+    }
     pf_fence_before();
-    __syncthreads();
+    if constexpr (kBounded) missing = __syncthreads_or(missing);
+    else __syncthreads();
     pf_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl->tmem_base);
 
@@ -577,6 +588,13 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             __syncwarp();
             if (lane == 0) pf_arrive(&ctl->q_full[t]);
         }
+        // bounded: a tile that starts at j0 is seen whole by all rows of the warp up to seen_to, and from behind seen_from or up to seen_sinks
+        int seen_to = 0, seen_from = 0, seen_sinks = 0;
+        if constexpr (kBounded) {
+            seen_to = (int)pos_warp - (C::kTile - 1);
+            seen_from = bounded.a.window ? (int)pos0 + (warp * 32 + 31) / R - bounded.a.window : -1;
+            seen_sinks = bounded.a.sinks - C::kTile;
+        }
         float m = -INFINITY, l = 0.f;                                       // reference of the weights (log2 domain), their sum
         bool ok = true;
         for (int jt = 0; jt < n_tiles; ++jt) {
@@ -594,21 +612,27 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             float* sb = reinterpret_cast<float*>(b);
             const int64_t j0 = (int64_t)tile_at(jt) * C::kTile;
             if constexpr (kBounded) {
-                const int window = bounded.a.window, sinks = bounded.a.sinks;
-                const int pos_most = (int)pos0 + (warp * 32 + 31) / R;      // largest position among the warp's rows
-                uint32_t holes = 0u;                                        // a byte per 16 tokens
-                if (bounded.a.page_table) {
-                    const int stage = jt % C::kStages;
-                    ok &= pf_wait(ctl, &ctl->full[stage], (uint32_t)(jt / C::kStages) & 1u);      // (long since: orders the read)
-                    holes = *reinterpret_cast<volatile uint32_t*>(&ctl->hole[stage][0]);
-                }
-                if (j0 + C::kTile - 1 > pos_warp || holes || (window && j0 <= pos_most - window && j0 + C::kTile > sinks)) {
-                    const int left = (int)(pos - j0);                       // columns 0 ... left are not in the future;
-                    const int out_from = window ? (sinks > j0 ? sinks - (int)j0 : 0) : C::kTile, out_to = left - window;      // from ... to are behind the window
+                if ((int)j0 > seen_to || ((int)j0 <= seen_from && (int)j0 > seen_sinks) || missing) {
+                    // bit i: this row sees column i
+                    const int left = (int)pos - (int)j0, window = bounded.a.window, sinks = bounded.a.sinks - (int)j0;
+                    uint64_t sees = left < 0 ? 0u : left >= 63 ? ~(uint64_t)0 : ((uint64_t)2 << left) - 1u;
+                    if (window && left - window >= 0) {                     // columns 0 ... left - window are behind the window, sinks apart
+                        const uint64_t behind = left - window >= 63 ? ~(uint64_t)0 : ((uint64_t)2 << (left - window)) - 1u;
+                        const uint64_t first = sinks <= 0 ? 0u : sinks >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << sinks) - 1u;
+                        sees &= ~behind | first;
+                    }
+                    if (missing) {
+                        const int stage = jt % C::kStages;
+                        ok &= pf_wait(ctl, &ctl->full[stage], (uint32_t)(jt / C::kStages) & 1u);      // (long since: it orders the read)
+                        const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&ctl->hole[stage][0]);      // a byte per 16 columns
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if ((holes >> (8 * i)) & 1u) sees &= ~((uint64_t)0xffffu << (16 * i));
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        if (i > left || (i >= out_from && i <= out_to) || ((holes >> (8 * (i >> 4))) & 1u)) sa[i] = -INFINITY;
-                        if (i + 32 > left || (i + 32 >= out_from && i + 32 <= out_to) || ((holes >> (16 + 8 * (i >> 4))) & 1u)) sb[i] = -INFINITY;
+                        if (!(((uint32_t)sees >> i) & 1u)) sa[i] = -INFINITY;
+                        if (!(((uint32_t)(sees >> 32) >> i) & 1u)) sb[i] = -INFINITY;
                     }
                 }
             } else if (j0 + C::kTile - 1 > pos_warp) {                      // some row's causal limit lies in the tile

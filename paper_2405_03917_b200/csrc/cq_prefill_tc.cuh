@@ -10,10 +10,13 @@ namespace cq {
 
 namespace {
 
-struct PfCfg {
+// kParts: softmax threads of a row, each with as many of its columns.
+template <int kParts>
+struct PfCfgT {
     static constexpr int kRows = 256;             // (query, head) rows per CTA: two tiles of 128, one tensor-memory lane each
-    static constexpr int kMmaWarp = 8;            // one thread issues the MMAs; the warps before it: softmax, four per row tile, a thread per row
-    static constexpr int kProducerWarp0 = 9, kProducerWarps = 4;       // dequantise the tiles
+    static constexpr int kSoftWarps = 8 * kParts; // softmax: four per row tile and part, a thread per row (and part)
+    static constexpr int kMmaWarp = kSoftWarps;   // one thread issues the MMAs
+    static constexpr int kProducerWarp0 = kMmaWarp + 1, kProducerWarps = 4;       // dequantise the tiles
     static constexpr int kSumWarp = kProducerWarp0 + kProducerWarps;
     static constexpr int kThreads = (kSumWarp + 1) * 32;
     static constexpr int kTile = 64;              // cached tokens per step
@@ -25,17 +28,21 @@ struct PfCfg {
     static constexpr int kVtOffset = 2 * kCbBytes;                     // [stages]
     static constexpr int kKtOffset = kVtOffset + kStages * kTileBytes; // [stages]
     static constexpr int kCtlOffset = kKtOffset + kStages * kTileBytes;
-    static constexpr int kSmemBytes = kCtlOffset + 256;                // 224.25 KiB
+    static constexpr int kExchangeOffset = kCtlOffset + 256;           // two parts: [part][row] what the threads of a row tell each other
+    static constexpr int kSmemBytes = kExchangeOffset + (kParts > 1 ? kParts * kRows * 4 : 0);      // 224.25 KiB, 226.25 with two parts
     // tensor-memory columns: output accumulators (fp32) and queries (fp16, two per column) of both row tiles, ONE tile of
     // scores (fp32) that the row tiles use in turn, weights (fp16) of both row tiles
     static constexpr int kOCol = 0, kQCol = 256, kSCol = 384, kPCol = 448;
     // where the set-up leaves the queries: behind stage 0, which the producers fill while they are read
     static constexpr int kOutStride = 144;        // bytes between the rows of a warp's 32 x 32 block of results (in the codebooks' place)
     __host__ __device__ static constexpr int q_offset(int rho) { return (rho < 128 ? kVtOffset : kKtOffset) + kTileBytes + (rho & 127) * 256; }
-    static_assert(kStages >= 3 && 8 * 32 * kOutStride <= 2 * kCbBytes, "room");
+    static_assert(kStages >= 3 && kSoftWarps * 32 * kOutStride <= 2 * kCbBytes, "room");
     static_assert(kKtOffset % 1024 == 0 && kTileBytes % 1024 == 0, "swizzled tiles");
     static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 };
+
+using PfCfg = PfCfgT<1>;
+using PfCfgB = PfCfgT<2>;                 // the bounded form
 
 constexpr int kPfLeastShare = 4;          // tiles of a CTA's part of a context, at least
 
@@ -156,6 +163,12 @@ __device__ __forceinline__ void pf_st32(uint32_t taddr, const uint32_t (&u)[32])
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
                  ::"r"(taddr), CQ_IN32(u) : "memory");
 }
+__device__ __forceinline__ void pf_st16(uint32_t taddr, const uint32_t (&u)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
+                 "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]) : "memory");
+}
 __device__ __forceinline__ void pf_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void pf_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void pf_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -197,8 +210,18 @@ __device__ __forceinline__ int pf_find_tile(const BoundedArgs& a, int index, int
     return -1;
 }
 
+// Of the threads of a warp pair (barrier `id`): whether any says so.
+__device__ __forceinline__ bool pf_pair_any(int id, bool q)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, r;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred r, %2, 64, p;\n\tselp.u32 %0, 1, 0, r;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)q), "r"(id) : "memory");
+    return any != 0;
+}
+__device__ __forceinline__ void pf_pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+
 template <int kC, class Bounded = PfNone>
-__global__ void __launch_bounds__(PfCfg::kThreads, 1)
+__global__ void __launch_bounds__(std::is_same<Bounded, PfNone>::value ? PfCfg::kThreads : PfCfgB::kThreads, 1)
 prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                   const float* __restrict__ kcb, const float* __restrict__ vcb,
                   const int32_t* __restrict__ seq_lens, float scale_log2e, Shape sh, int n_q, int row_tiles,
@@ -207,7 +230,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
     constexpr bool kBounded = !std::is_same<Bounded, PfNone>::value;
     asm volatile("griddepcontrol.wait;" ::: "memory");      // launched ahead of the end of the kernel before it, and
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the kernel behind it ahead of its own
-    using C = PfCfg;
+    using C = typename std::conditional<kBounded, PfCfgB, PfCfg>::type;
     constexpr int G = 128 / kC;
     extern __shared__ __align__(1024) uint8_t smem[];
     PfCtl* ctl = reinterpret_cast<PfCtl*>(smem + C::kCtlOffset);
@@ -269,8 +292,6 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
     const uint32_t q_sign = scale_log2e < 0.f ? 0x80008000u : 0u, q_keep = scale_log2e == 0.f ? 0u : 0xffffffffu;
     const float scale = scale_log2e == 0.f ? 1.f : fabsf(scale_log2e);
 
-    int bounded_parts = 1;
-    if constexpr (kBounded) bounded_parts = bounded.parts;
     const int rows_used = q_per_tile * R;                                  // (bounded: R need not divide 256)
 
     // ---- barriers, tensor memory
@@ -281,9 +302,9 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
         }
         for (int t = 0; t < 2; ++t) {
             pf_init(&ctl->s_full[t], 1);
-            pf_init(&ctl->s_free[t], 4);
-            pf_init(&ctl->q_full[t], 4);
-            pf_init(&ctl->p_full[t], 4);
+            pf_init(&ctl->s_free[t], C::kSoftWarps / 2);
+            pf_init(&ctl->q_full[t], C::kSoftWarps / 2);
+            pf_init(&ctl->p_full[t], C::kSoftWarps / 2);
             pf_init(&ctl->pv_done[t], 1);
             pf_init(&ctl->drained[t], 1);
         }
@@ -562,13 +583,181 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             __syncwarp();
             pf_drain(&ctl->drained[1]);
         }
+    } else if constexpr (kBounded) {
+        // ---------------------------------------------------------------- softmax: two threads per row, 32 columns each.  (A thread per row
+        // took some 2000 cycles for its 64 columns, as long as everything else in two tiles; half the exponentials on the FMA pipe instead
+        // of the special-function unit made that longer still: it is latencies that a single thread cannot hide.)  The threads of a
+        // row are in two warps, which agree on the reference of the weights; only when it moves do they exchange maxima.
+        const int part = warp >> 3, t = (warp >> 2) & 1;
+        if (warp < C::kSoftWarps && t < n_halves) {
+            const int row0 = t * 128 + (warp & 3) * 32, rho = row0 + lane, pair = 1 + (warp & 7);
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            const uint32_t s_addr = lanes + C::kSCol + 32 * part, p_addr = lanes + C::kPCol + 32 * t + 16 * part, o_addr = lanes + C::kOCol + 128 * t + 64 * part;
+            volatile float* exchange = reinterpret_cast<float*>(smem + C::kExchangeOffset);
+            const int qi = qi0 + rho / R, window = bounded.a.window;
+            const int pos = qi < n_q && rho < rows_used ? (int)pos0 + rho / R : -1;
+            // a tile part that starts at j0 is seen whole by all rows of the warp up to seen_to, and from behind seen_from or up to seen_sinks
+            const int seen_to = (int)pos0 + row0 / R - 31, seen_from = window ? (int)pos0 + (row0 + 31) / R - window : -1, seen_sinks = bounded.a.sinks - 32;
+            {
+                uint32_t u[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(smem + C::q_offset(rho) + (((8 * part + i) ^ (rho & 7)) << 4));
+                    u[4 * i] = (v.x ^ q_sign) & q_keep; u[4 * i + 1] = (v.y ^ q_sign) & q_keep;
+                    u[4 * i + 2] = (v.z ^ q_sign) & q_keep; u[4 * i + 3] = (v.w ^ q_sign) & q_keep;
+                }
+                pf_st32(lanes + C::kQCol + 64 * t + 32 * part, u);
+                pf_st_wait();
+                pf_fence_before();
+                __syncwarp();
+                if (lane == 0) pf_arrive(&ctl->q_full[t]);
+            }
+            float m = -INFINITY, l = 0.f;                                   // reference of the weights (log2 domain), the sum of this thread's
+            bool ok = true;
+#pragma unroll 1
+            for (int jt = 0; jt < n_tiles; ++jt) {
+                ok &= pf_wait(ctl, &ctl->s_full[t], (uint32_t)jt & 1u);
+                pf_fence_after();
+                uint32_t a[32];
+                pf_ld32(a, s_addr);
+                pf_ld_wait(a);
+                pf_fence_before();
+                __syncwarp();
+                if (lane == 0) pf_arrive(&ctl->s_free[t]);
+                float* sa = reinterpret_cast<float*>(a);
+                const int j0 = tile_at(jt) * C::kTile + 32 * part;
+                if (j0 > seen_to || (j0 <= seen_from && j0 > seen_sinks) || missing) {
+                    // bit i: this row sees column i
+                    const int left = pos - j0, sinks = bounded.a.sinks - j0;
+                    uint32_t sees = left < 0 ? 0u : left >= 31 ? ~0u : (2u << left) - 1u;
+                    if (window && left - window >= 0) {                     // columns 0 ... left - window are behind the window, sinks apart
+                        const uint32_t behind = left - window >= 31 ? ~0u : (2u << (left - window)) - 1u;
+                        const uint32_t first = sinks <= 0 ? 0u : sinks >= 32 ? ~0u : (1u << sinks) - 1u;
+                        sees &= ~behind | first;
+                    }
+                    if (missing) {
+                        const int stage = jt % C::kStages;
+                        ok &= pf_wait(ctl, &ctl->full[stage], (uint32_t)(jt / C::kStages) & 1u);      // (long since: it orders the read)
+                        const volatile uint8_t* holes = &ctl->hole[stage][2 * part];
+                        if (holes[0]) sees &= 0xffff0000u;
+                        if (holes[1]) sees &= 0x0000ffffu;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!((sees >> i) & 1u)) sa[i] = -INFINITY;
+                }
+                float mx[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = max3(sa[k], sa[k + 4], sa[k + 8]);
+#pragma unroll
+                for (int i = 12; i < 28; i += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], sa[i + k], sa[i + 4 + k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], sa[28 + k]);
+                const float m_tile = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * scale;      // (-inf: the row sees nothing of this part)
+                // The reference follows the maximum only when it is more than 8 (a factor of 256) behind: the sums rarely have to be
+                // rescaled, and fp16 weights up to 256 are as precise as weights up to 1.
+                const bool rescale = pf_pair_any(pair, m_tile > m + 8.f || (m == -INFINITY && m_tile > -INFINITY));
+                float f = 1.f;
+                if (rescale) {
+                    exchange[part * C::kRows + rho] = m_tile;
+                    pf_pair_sync(pair);
+                    const float m_new = max3(m, m_tile, exchange[(part ^ 1) * C::kRows + rho]);
+                    pf_pair_sync(pair);
+                    f = m == -INFINITY ? 0.f : exp2f(m - m_new);
+                    m = m_new;
+                    l *= f;
+                }
+                const float mm = m == -INFINITY ? 0.f : m;
+                uint32_t p[16];
+                float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x0 = ex2_approx(fmaf(sa[2 * i], scale, -mm)), x1 = ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
+                    l0 += x0;
+                    l1 += x1;
+                    p[i] = pack_half2(x0, x1);
+                }
+                l += l0 + l1;
+                if (jt > 0) {                                               // the last sums are done with the weights' columns
+                    ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(jt - 1) & 1u);
+                    pf_fence_after();
+                    if (rescale) {
+#pragma unroll 1
+                        for (int c0 = 0; c0 < 64; c0 += 32) {
+                            uint32_t o[32];
+                            pf_ld32(o, o_addr + c0);
+                            pf_ld_wait(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            pf_st32(o_addr + c0, o);
+                        }
+                    }
+                }
+                pf_st16(p_addr, p);
+                pf_st_wait();
+                pf_fence_before();
+                __syncwarp();
+                if (lane == 0) pf_arrive(&ctl->p_full[t]);
+            }
+            exchange[part * C::kRows + rho] = l;
+            pf_pair_sync(pair);
+            l += exchange[(part ^ 1) * C::kRows + rho];
+            // ---- normalise and write, through shared memory (the codebooks are done with when the last sums are), in whole lines
+            if (n_tiles > 0) ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(n_tiles - 1) & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            pf_fence_after();
+            const bool partial = bounded.parts > 1;                         // (partials: the accumulators as they are)
+            // nothing seen: a zero row; a wait gave up: NaN rows, so that nothing takes them for a result
+            const float inv = !ok ? __int_as_float(0x7fffffff) : partial ? 1.f : l > 0.f ? 1.f / l : 0.f;
+            float* to_part = nullptr;
+            if (partial) {
+                to_part = bounded.partials + ((int64_t)blockIdx.x * C::kRows + row0) * partial_stride(128);
+                if (part == 0) {
+                    to_part[lane * partial_stride(128)] = m;
+                    to_part[lane * partial_stride(128) + 1] = l;
+                }
+            }
+            uint8_t* block = smem + warp * 32 * C::kOutStride;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 64; c0 += 32) {
+                uint32_t o[32];
+                if (n_tiles > 0) {
+                    pf_ld32(o, o_addr + c0);
+                    pf_ld_wait(o);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<float4*>(block + lane * C::kOutStride + 16 * i) =
+                        inv == 0.f || n_tiles == 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                   : make_float4(__uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
+                                                                 __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int rw = 4 * i + (lane >> 3), rr = row0 + rw, qr = qi0 + rr / R, column = 64 * part + c0 + 4 * (lane & 7);
+                    const float4 v = *reinterpret_cast<const float4*>(block + rw * C::kOutStride + 16 * (lane & 7));
+                    if (partial) {
+                        float* to = to_part + rw * partial_stride(128) + 2 + column;
+                        *reinterpret_cast<float2*>(to) = make_float2(v.x, v.y);
+                        *reinterpret_cast<float2*>(to + 2) = make_float2(v.z, v.w);
+                    } else if (qr < n_q && rr < rows_used) {
+                        *reinterpret_cast<uint2*>(bounded.a.out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + column) =
+                            make_uint2(pack_half2(v.x, v.y), pack_half2(v.z, v.w));
+                    }
+                }
+                __syncwarp();
+            }
+            pf_fence_before();
+        }
     } else if (warp < 4 * n_halves) {
         // ---------------------------------------------------------------- softmax: a thread per row
         const int t = warp >> 2, rho = threadIdx.x;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_addr = lanes + C::kSCol, p_addr = lanes + C::kPCol + 32 * t, o_addr = lanes + C::kOCol + 128 * t;
         const int qi = qi0 + rho / R;
-        const bool live = qi < n_q && (!kBounded || rho < rows_used);
+        const bool live = qi < n_q;
         const int64_t pos = live ? pos0 + rho / R : -1;
         const int64_t pos_warp = pos0 + (warp * 32) / R;                   // smallest position among the warp's rows
         {
@@ -588,13 +777,6 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             __syncwarp();
             if (lane == 0) pf_arrive(&ctl->q_full[t]);
         }
-        // bounded: a tile that starts at j0 is seen whole by all rows of the warp up to seen_to, and from behind seen_from or up to seen_sinks
-        int seen_to = 0, seen_from = 0, seen_sinks = 0;
-        if constexpr (kBounded) {
-            seen_to = (int)pos_warp - (C::kTile - 1);
-            seen_from = bounded.a.window ? (int)pos0 + (warp * 32 + 31) / R - bounded.a.window : -1;
-            seen_sinks = bounded.a.sinks - C::kTile;
-        }
         float m = -INFINITY, l = 0.f;                                       // reference of the weights (log2 domain), their sum
         bool ok = true;
         for (int jt = 0; jt < n_tiles; ++jt) {
@@ -610,32 +792,8 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             if (lane == 0) pf_arrive(&ctl->s_free[t]);
             float* sa = reinterpret_cast<float*>(a);
             float* sb = reinterpret_cast<float*>(b);
-            const int64_t j0 = (int64_t)tile_at(jt) * C::kTile;
-            if constexpr (kBounded) {
-                if ((int)j0 > seen_to || ((int)j0 <= seen_from && (int)j0 > seen_sinks) || missing) {
-                    // bit i: this row sees column i
-                    const int left = (int)pos - (int)j0, window = bounded.a.window, sinks = bounded.a.sinks - (int)j0;
-                    uint64_t sees = left < 0 ? 0u : left >= 63 ? ~(uint64_t)0 : ((uint64_t)2 << left) - 1u;
-                    if (window && left - window >= 0) {                     // columns 0 ... left - window are behind the window, sinks apart
-                        const uint64_t behind = left - window >= 63 ? ~(uint64_t)0 : ((uint64_t)2 << (left - window)) - 1u;
-                        const uint64_t first = sinks <= 0 ? 0u : sinks >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << sinks) - 1u;
-                        sees &= ~behind | first;
-                    }
-                    if (missing) {
-                        const int stage = jt % C::kStages;
-                        ok &= pf_wait(ctl, &ctl->full[stage], (uint32_t)(jt / C::kStages) & 1u);      // (long since: it orders the read)
-                        const uint32_t holes = *reinterpret_cast<volatile uint32_t*>(&ctl->hole[stage][0]);      // a byte per 16 columns
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if ((holes >> (8 * i)) & 1u) sees &= ~((uint64_t)0xffffu << (16 * i));
-                    }
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (!(((uint32_t)sees >> i) & 1u)) sa[i] = -INFINITY;
-                        if (!(((uint32_t)(sees >> 32) >> i) & 1u)) sb[i] = -INFINITY;
-                    }
-                }
-            } else if (j0 + C::kTile - 1 > pos_warp) {                      // some row's causal limit lies in the tile
+            const int64_t j0 = (int64_t)jt * C::kTile;
+            if (j0 + C::kTile - 1 > pos_warp) {                             // some row's causal limit lies in the tile
                 const int64_t left = pos - j0;                              // columns 0 ... left are attended
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
@@ -714,16 +872,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
         ok = __all_sync(0xffffffffu, ok);
         pf_fence_after();
         // no position: zero row; a wait gave up: NaN rows, so that nothing takes them for a result
-        const bool partial = kBounded && bounded_parts > 1;                 // (partials: the accumulators as they are)
-        const float inv = !ok ? __int_as_float(0x7fffffff) : partial ? 1.f : l > 0.f ? 1.f / l : 0.f;
-        float* part = nullptr;
-        if constexpr (kBounded) {
-            if (partial) {
-                part = bounded.partials + ((int64_t)blockIdx.x * C::kRows + warp * 32) * partial_stride(128);
-                part[lane * partial_stride(128)] = m;
-                part[lane * partial_stride(128) + 1] = l;
-            }
-        }
+        const float inv = !ok ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : 0.f;
         uint8_t* block = smem + warp * 32 * C::kOutStride;
 #pragma unroll 1
         for (int c0 = 0; c0 < 128; c0 += 32) {
@@ -735,26 +884,16 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 *reinterpret_cast<float4*>(block + lane * C::kOutStride + 16 * i) =
-                    inv == 0.f || n_tiles == 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                    inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
                                : make_float4(__uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
                                              __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int rw = 4 * i + (lane >> 3), rr = warp * 32 + rw, qr = qi0 + rr / R;
-                const float4 v = *reinterpret_cast<const float4*>(block + rw * C::kOutStride + 16 * (lane & 7));
-                if constexpr (kBounded) {
-                    if (partial) {
-                        float* to = part + rw * partial_stride(128) + 2 + c0 + 4 * (lane & 7);
-                        *reinterpret_cast<float2*>(to) = make_float2(v.x, v.y);
-                        *reinterpret_cast<float2*>(to + 2) = make_float2(v.z, v.w);
-                    } else if (qr < n_q && rr < rows_used) {
-                        *reinterpret_cast<uint2*>(bounded.a.out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + c0 + 4 * (lane & 7)) =
-                            make_uint2(pack_half2(v.x, v.y), pack_half2(v.z, v.w));
-                    }
-                } else if (qr < n_q) {
-                    *reinterpret_cast<float4*>(out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + c0 + 4 * (lane & 7)) = v;
-                }
+                if (qr < n_q)
+                    *reinterpret_cast<float4*>(out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + c0 + 4 * (lane & 7)) =
+                        *reinterpret_cast<const float4*>(block + rw * C::kOutStride + 16 * (lane & 7));
             }
             __syncwarp();
         }

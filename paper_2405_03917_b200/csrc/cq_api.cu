@@ -11,7 +11,7 @@ namespace cq {
 
 namespace {
 constexpr int kMaxHeadDim = 256;
-constexpr int kDeviceSlots = 64, kSmemSlots = 128;
+constexpr int kDeviceSlots = 64, kSmemSlots = 192;
 std::mutex g_device_mutex;
 int g_sm_count[kDeviceSlots] = {};                   // 0: not queried yet
 int g_smem_set[kDeviceSlots][kSmemSlots] = {};               // per device and call site: dynamic shared memory size already set

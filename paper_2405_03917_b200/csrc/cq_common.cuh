@@ -74,7 +74,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // SM count of the current device (queried once per device and process).
 int device_sm_count();
 // cudaFuncAttributeMaxDynamicSharedMemorySize for `func`, set once per device and (func, bytes);
-// `slot` is a small integer unique to the call site (0 <= slot < 128).
+// `slot` is a small integer unique to the call site (0 <= slot < 192).
 cudaError_t ensure_dynamic_smem(const void* func, int bytes, int slot);
 
 // Launch plan of one tuned decode call: context chunk per CTA, partial slots per (sequence, query

@@ -909,7 +909,7 @@ size_t gather_bytes(int mode)
 int mass_row_stride(const BoundedArgs& a) { return (a.max_q * a.sh.R + 7) / 8 * 8; }
 
 template <int kMode>
-cudaError_t launch_mode(const BoundedArgs& a, const MassArgs& mass, void* workspace, int slot, cudaStream_t st)
+cudaError_t launch_mode(const BoundedArgs& a, const MassArgs& mass, void* workspace, int slot, cudaStream_t st)      // call-site slots from `slot` on: six
 {
     // Tiles of four rows where a query token has that few heads, otherwise of eight: with four rows no two lanes meet in a bank.
     // (Masses of many rows go over the keys once per tile: eight rows at a time from 16 rows on.)
@@ -924,7 +924,7 @@ cudaError_t launch_mode(const BoundedArgs& a, const MassArgs& mass, void* worksp
 bool gather_attn_supported(const Shape& sh) { return sh.head_dim == 128 && sh.b <= 8 && (sh.c == 2 || sh.c == 4 || sh.c == 8); }
 
 size_t gather_attn_workspace_bytes() { return gather_bytes(kAttn); }
-cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st) { return launch_mode<kAttn>(a, MassArgs(), workspace, 100, st); }
+cudaError_t launch_gather_attn(const BoundedArgs& a, void* workspace, cudaStream_t st) { return launch_mode<kAttn>(a, MassArgs(), workspace, 128, st); }
 
 namespace {
 size_t lse_bytes(const BoundedArgs& a) { return gather_bytes(kLse) + round_up((size_t)a.sh.n_seq * a.sh.n_kv_heads * mass_row_stride(a) * sizeof(float), 256); }
@@ -944,9 +944,9 @@ cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float
     mass.row_stride = mass_row_stride(a);
     const bool store = score_bytes(a) && workspace_bytes >= gather_mass_workspace_bytes(a);
     mass.scores = store ? reinterpret_cast<float*>(static_cast<char*>(workspace) + lse_bytes(a)) : nullptr;
-    const cudaError_t e = launch_mode<kLse>(a, mass, workspace, 109, st);
+    const cudaError_t e = launch_mode<kLse>(a, mass, workspace, 134, st);
     if (e != cudaSuccess) return e;
-    if (!store) return launch_mode<kMass>(a, mass, workspace, 115, st);
+    if (!store) return launch_mode<kMass>(a, mass, workspace, 140, st);
     const int64_t chunks = (a.sh.max_tokens + kStreamThreads * kStreamEach - 1) / (kStreamThreads * kStreamEach), grid = a.sh.n_seq * a.sh.n_kv_heads * chunks;
     if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
     cudaLaunchAttribute attr;

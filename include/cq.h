@@ -522,7 +522,7 @@ int cq_paged_append(const void *k_fp16, const void *v_fp16, const int32_t *q_off
  *                KV head) they hold the scores between the two passes, 16 bytes per cached token and KV head.  What the same call
  *                with max_tokens = n_q_tokens asks for is enough: the second pass then works the scores out again
  * Sums are formed in a fixed order: two calls on the same inputs give the same bits.
- * variant: 0 = automatic, 1 = plain kernels, 2 = tensor-core kernel (head_dim 128, one byte per code, c = 2, 4 or 8).
+ * variant: as above (up to 16 rows of a sequence and KV head take the gather kernel, more the tcgen05 one).
  */
 size_t cq_attn_mass_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b,
                                     int64_t max_tokens);

@@ -110,6 +110,9 @@ cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float
 bool chunk_attn_supported(const Shape& sh);
 size_t chunk_attn_workspace_bytes(const BoundedArgs& a);
 cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
+// the masses that they give (uniform rows, a contiguous cache, no window)
+size_t chunk_mass_workspace_bytes(const BoundedArgs& a);
+cudaError_t launch_chunk_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st);
 
 // the heaviest tokens of a cache to the front of another (cq_evict.cu)
 struct EvictArgs {

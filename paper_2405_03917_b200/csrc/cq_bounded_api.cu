@@ -203,18 +203,30 @@ int cq_paged_append(const void* k_fp16, const void* v_fp16, const int32_t* q_off
                                         static_cast<cudaStream_t>(stream)));
 }
 
-static size_t mass_workspace(const BoundedArgs& a, bool least)
+namespace {
+// Kernel of a call: 1 plain, 2 gather, 3 tensor cores (where the variant leaves it open: by the rows of a sequence).
+int mass_kernel(const BoundedArgs& a, int variant)
 {
-    const size_t plain = round_up((size_t)a.n_rows * a.sh.n_q_heads * sizeof(float), 256);
-    const size_t tuned = !gather_attn_supported(a.sh) ? 0 : least ? gather_mass_least_bytes(a) : gather_mass_workspace_bytes(a);
-    return plain > tuned ? plain : tuned;
+    if (variant != 0) return variant;
+    if (!gather_attn_supported(a.sh) || !chunk_attn_supported(a.sh)) return 1;
+    return (int64_t)a.max_q * a.sh.R <= kFewRows ? 2 : 3;
 }
+size_t mass_workspace(const BoundedArgs& a, int kernel, bool least)
+{
+    if (kernel == 2) return least ? gather_mass_least_bytes(a) : gather_mass_workspace_bytes(a);
+    if (kernel == 3) return chunk_mass_workspace_bytes(a);
+    return round_up((size_t)a.n_rows * a.sh.n_q_heads * sizeof(float), 256);
+}
+}  // namespace
 
 size_t cq_attn_mass_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, int n_kv_heads, int head_dim, int c, int b, int64_t max_tokens)
 {
     BoundedArgs a;
     if (bounded_shape(n_seq, (int64_t)n_seq * n_q_tokens, n_q_tokens, max_tokens, n_q_heads, n_kv_heads, head_dim, c, b, 0, 0, &a) != CQ_OK) return 0;
-    return mass_workspace(a, false);
+    size_t bytes = mass_workspace(a, 1, false);                                // enough for every kernel that the shape has
+    if (gather_attn_supported(a.sh) && mass_workspace(a, 2, false) > bytes) bytes = mass_workspace(a, 2, false);
+    if (chunk_attn_supported(a.sh) && mass_workspace(a, 3, false) > bytes) bytes = mass_workspace(a, 3, false);
+    return bytes;
 }
 
 int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_cb_fp16, const int32_t* seq_lens, float scale,
@@ -228,15 +240,17 @@ int cq_attn_mass_variant(const void* q_fp16, const void* k_codes, const void* k_
     if (!aligned16(q_fp16) || !aligned16(k_codes) || !aligned16(k_cb_fp16) || !aligned16(workspace) || !aligned4(seq_lens) || !aligned4(mass_in) ||
         !aligned4(mass_out))
         return CQ_ERR_ALIGN;
-    if (workspace_bytes < mass_workspace(a, true)) return CQ_ERR_WORKSPACE;
-    if (variant < 0 || variant > 2) return CQ_ERR_SHAPE;
-    if (variant == 2 && !gather_attn_supported(a.sh)) return CQ_ERR_UNSUPPORTED;
+    if (variant < 0 || variant > 3) return CQ_ERR_SHAPE;
+    if ((variant == 2 && !gather_attn_supported(a.sh)) || (variant == 3 && !chunk_attn_supported(a.sh))) return CQ_ERR_UNSUPPORTED;
+    const int kernel = mass_kernel(a, variant);
+    if (workspace_bytes < mass_workspace(a, kernel, true)) return CQ_ERR_WORKSPACE;
     a.q = static_cast<const __half*>(q_fp16);
     a.kc = static_cast<const uint8_t*>(k_codes);
     a.kcb = static_cast<const __half*>(k_cb_fp16);
     a.seq_lens = seq_lens;
     a.scale_log2e = scale * kLog2e;
-    if (variant != 1 && gather_attn_supported(a.sh)) return status(launch_gather_mass(a, mass_in, mass_out, workspace, workspace_bytes, static_cast<cudaStream_t>(stream)));
+    if (kernel == 2) return status(launch_gather_mass(a, mass_in, mass_out, workspace, workspace_bytes, static_cast<cudaStream_t>(stream)));
+    if (kernel == 3) return status(launch_chunk_mass(a, mass_in, mass_out, workspace, static_cast<cudaStream_t>(stream)));
     return status(launch_mass_plain(a, mass_in, mass_out, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }
 

@@ -1,5 +1,5 @@
-// Attention of many query rows over a bounded cache (window, sinks, pages, ragged rows): the bounded form of the tensor-core kernel in
-// cq_prefill_tc.cuh, and the merge of contexts that several CTAs share.
+// Attention of many query rows over a bounded cache (window, sinks, pages, ragged rows), and the masses that they give to cached tokens:
+// the bounded forms of the tensor-core kernel in cq_prefill_tc.cuh, and what joins the parts of a context or the row tiles.
 #include "cq_prefill_tc.cuh"
 
 namespace cq {
@@ -9,7 +9,7 @@ namespace {
 constexpr int kMergeWarps = 8;
 
 // A warp per row of a row tile: log-sum-exp merge of the parts' accumulators.
-__global__ void __launch_bounds__(kMergeWarps * 32) chunk_merge_kernel(PfBounded b)
+__global__ void __launch_bounds__(kMergeWarps * 32) chunk_merge_kernel(PfBounded<kPfAttn> b)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const BoundedArgs& a = b.a;
@@ -79,29 +79,98 @@ size_t chunk_attn_workspace_bytes(const BoundedArgs& a)
     return p.parts == 1 ? 0 : (size_t)(p.tiles * a.sh.n_kv_heads * p.parts) * PfCfgB::kRows * partial_stride(128) * sizeof(float);
 }
 
+namespace {
+
+template <int kWhat>
+cudaError_t launch_kernel(const PfBounded<kWhat>& b, int64_t items, int slot, cudaStream_t st)
+{
+    const BoundedArgs& a = b.a;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = overlapped_config((unsigned)(items * b.parts), PfCfgB::kThreads, PfCfgB::kSmemBytes, st, &attr);
+    auto go = [&](auto kernel, int at) {
+        const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), PfCfgB::kSmemBytes, at);
+        if (e != cudaSuccess) return e;
+        return cudaLaunchKernelEx(&cfg, kernel, a.q, a.kc, a.vc, (const float*)nullptr, (const float*)nullptr, a.seq_lens, a.scale_log2e, a.sh, a.max_q, 0,
+                                  (float*)nullptr, b);
+    };
+    return a.sh.c == 8 ? go(prefill_tc_kernel<8, PfBounded<kWhat>>, slot) : a.sh.c == 4 ? go(prefill_tc_kernel<4, PfBounded<kWhat>>, slot + 1)
+                                                                                        : go(prefill_tc_kernel<2, PfBounded<kWhat>>, slot + 2);
+}
+
+// Masses of several row tiles: a thread per token adds those of the tiles that see it, the earliest queries' first.
+__global__ void __launch_bounds__(256) mass_sum_kernel(BoundedArgs a, const float* __restrict__ sums, int row_tiles, int chunks, const float* mass_in,
+                                                       float* mass_out)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t item = blockIdx.x / chunks;
+    const int t = (int)(blockIdx.x % chunks) * 256 + (int)threadIdx.x;
+    const SeqView sv = seq_view(a, (int)(item / a.sh.n_kv_heads));
+    if (t >= sv.n) return;
+    const int q_per_tile = PfCfgB::kRows / a.sh.R;
+    const int64_t at = item * a.sh.max_tokens + t, stride = a.sh.n_seq * a.sh.n_kv_heads * a.sh.max_tokens;
+    float sum = 0.f;
+    for (int i = 0; i < row_tiles; ++i) {
+        const int last = (i + 1) * q_per_tile < sv.m ? (i + 1) * q_per_tile - 1 : sv.m - 1;       // the tile's last query; it wrote whole tiles of tokens
+        if ((sv.n - sv.m + last) / PfCfgB::kTile >= t / PfCfgB::kTile && sv.n - sv.m + last >= 0) sum += sums[i * stride + at];
+    }
+    mass_out[at] = (mass_in ? mass_in[at] : 0.f) + sum;
+}
+
+size_t lse_bytes(const BoundedArgs& a, const Plan& p) { return round_up((size_t)(p.tiles * a.sh.n_kv_heads * p.parts) * PfCfgB::kRows * 2 * sizeof(float), 256); }
+int row_tiles_of(const BoundedArgs& a) { const int q_per_tile = PfCfgB::kRows / a.sh.R; return (a.max_q + q_per_tile - 1) / q_per_tile; }
+
+}  // namespace
+
 cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, cudaStream_t st)
 {
     const Plan p = plan_of(a);
     const int64_t items = p.tiles * a.sh.n_kv_heads;
     if (items * p.parts > 0x7fffffff || items * (PfCfgB::kRows / kMergeWarps) > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    PfBounded b;
+    PfBounded<kPfAttn> b = {};
     b.a = a;
     b.tiles = (int)p.tiles;
     b.parts = p.parts;
     b.partials = static_cast<float*>(workspace);
-    cudaLaunchAttribute attr;
-    cudaLaunchConfig_t cfg = overlapped_config((unsigned)(items * p.parts), PfCfgB::kThreads, PfCfgB::kSmemBytes, st, &attr);
-    auto go = [&](auto kernel, int slot) {
-        const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), PfCfgB::kSmemBytes, slot);
-        if (e != cudaSuccess) return e;
-        return cudaLaunchKernelEx(&cfg, kernel, a.q, a.kc, a.vc, (const float*)nullptr, (const float*)nullptr, a.seq_lens, a.scale_log2e, a.sh, a.max_q, 0,
-                                  (float*)nullptr, b);
-    };
-    cudaError_t e = a.sh.c == 8 ? go(prefill_tc_kernel<8, PfBounded>, 106) : a.sh.c == 4 ? go(prefill_tc_kernel<4, PfBounded>, 107)
-                                                                                         : go(prefill_tc_kernel<2, PfBounded>, 108);
+    const cudaError_t e = launch_kernel(b, items, 146, st);
     if (e != cudaSuccess || p.parts == 1) return e;
-    cfg = overlapped_config((unsigned)(items * (PfCfgB::kRows / kMergeWarps)), kMergeWarps * 32, 0, st, &attr);
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = overlapped_config((unsigned)(items * (PfCfgB::kRows / kMergeWarps)), kMergeWarps * 32, 0, st, &attr);
     return cudaLaunchKernelEx(&cfg, chunk_merge_kernel, b);
+}
+
+size_t chunk_mass_workspace_bytes(const BoundedArgs& a)
+{
+    const int row_tiles = row_tiles_of(a);
+    return lse_bytes(a, plan_of(a)) + (row_tiles > 1 ? (size_t)row_tiles * a.sh.n_seq * a.sh.n_kv_heads * a.sh.max_tokens * sizeof(float) : 0);
+}
+
+cudaError_t launch_chunk_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st)
+{
+    const Plan p = plan_of(a);
+    const int64_t items = p.tiles * a.sh.n_kv_heads, chunks = (a.sh.max_tokens + 255) / 256, sum_grid = a.sh.n_seq * a.sh.n_kv_heads * chunks;
+    if (items * p.parts > 0x7fffffff || sum_grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    PfBounded<kPfLse> b = {};
+    b.a = a;
+    b.tiles = (int)p.tiles;
+    b.parts = p.parts;
+    b.partials = static_cast<float*>(workspace);
+    b.row_tiles = row_tiles_of(a);
+    cudaError_t e = launch_kernel(b, items, 149, st);
+    if (e != cudaSuccess) return e;
+    PfBounded<kPfMass> c = {};
+    c.a = a;
+    c.tiles = b.tiles;
+    c.parts = b.parts;
+    c.partials = b.partials;
+    c.row_tiles = b.row_tiles;
+    c.mass_in = mass_in;
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + lse_bytes(a, p));
+    c.mass_out = c.row_tiles > 1 ? sums : mass_out;
+    e = launch_kernel(c, items, 152, st);
+    if (e != cudaSuccess || c.row_tiles == 1) return e;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = overlapped_config((unsigned)sum_grid, 256, 0, st, &attr);
+    return cudaLaunchKernelEx(&cfg, mass_sum_kernel, a, (const float*)sums, c.row_tiles, (int)chunks, mass_in, mass_out);
 }
 
 }  // namespace cq

@@ -173,13 +173,24 @@ __device__ __forceinline__ void pf_st_wait() { asm volatile("tcgen05.wait::st.sy
 __device__ __forceinline__ void pf_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void pf_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// The bounded form: windows, sinks, pages, ragged rows, fp16 codebooks and results, contexts split over CTAs.
-struct PfNone {};
+// The bounded form: windows, sinks, pages, ragged rows, fp16 codebooks and results, contexts split over CTAs.  kPfLse and kPfMass do the
+// scores alone: the first leaves the log-sum-exp of every row, as (reference, sum) of every part of its context; the second adds up,
+// per token, the weights of a row tile's rows.
+enum PfWhat { kPfNone, kPfAttn, kPfLse, kPfMass };
+struct PfNone {
+    static constexpr int kWhat = kPfNone;
+};
+template <int kWhatFor>
 struct PfBounded {
+    static constexpr int kWhat = kWhatFor;
     BoundedArgs a;
     int tiles;                 // bound on the row tiles of all sequences
     int parts;                 // CTAs that share a row tile's context
-    float* partials;           // parts > 1: [CTA][256 rows][partial_stride(128)] (reference, sum, accumulators)
+    float* partials;           // attention, parts > 1: [CTA][256 rows][partial_stride(128)] (reference, sum, accumulators);
+                               // log-sum-exps: [CTA][256 rows][2]
+    const float* mass_in;      // masses: of one row tile per sequence, on top of these (may be null)
+    float* mass_out;           // [sequence][KV head][max_tokens]; of several row tiles, [row tile][sequence][KV head][max_tokens]
+    int row_tiles;
 };
 // Row tiles of a sequence.
 __device__ __forceinline__ int pf_tiles_of(const BoundedArgs& a, const SeqView& v, int q_per_tile)
@@ -221,13 +232,14 @@ __device__ __forceinline__ bool pf_pair_any(int id, bool q)
 __device__ __forceinline__ void pf_pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
 template <int kC, class Bounded = PfNone>
-__global__ void __launch_bounds__(std::is_same<Bounded, PfNone>::value ? PfCfg::kThreads : PfCfgB::kThreads, 1)
+__global__ void __launch_bounds__(Bounded::kWhat == kPfNone ? PfCfg::kThreads : PfCfgB::kThreads, 1)
 prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                   const float* __restrict__ kcb, const float* __restrict__ vcb,
                   const int32_t* __restrict__ seq_lens, float scale_log2e, Shape sh, int n_q, int row_tiles,
                   float* __restrict__ out, Bounded bounded)
 {
-    constexpr bool kBounded = !std::is_same<Bounded, PfNone>::value;
+    constexpr int kWhat = Bounded::kWhat;
+    constexpr bool kBounded = kWhat != kPfNone, kSums = kWhat == kPfNone || kWhat == kPfAttn;      // kSums: values and their sums
     asm volatile("griddepcontrol.wait;" ::: "memory");      // launched ahead of the end of the kernel before it, and
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the kernel behind it ahead of its own
     using C = typename std::conditional<kBounded, PfCfgB, PfCfg>::type;
@@ -332,7 +344,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
     // met eight at a time, took 12.7 thousand cycles per CTA; 4 thousand are what the L2 takes to deliver 256 KB.)
     if constexpr (kBounded) {
         // fp16 as they come: a warp takes four centroids' 64 bytes (c = 8) of eight groups, a quarter of it two groups
-        constexpr int kTasks = 2 * (G / 8) * (64 * kC / 8), kBatch = 6, kWarps = C::kThreads / 32, kHalves = kTasks / 2;
+        constexpr int kHalves = (G / 8) * (64 * kC / 8), kTasks = kSums ? 2 * kHalves : kHalves, kBatch = 6, kWarps = C::kThreads / 32;
         const int gl = lane >> 2, j = lane & 3, pieces = sh.K * kC / 8;     // 16-byte pieces of a group's codebook
 #pragma unroll 1
         for (int i0 = warp; i0 < kTasks; i0 += kBatch * kWarps) {
@@ -444,18 +456,29 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             const uint8_t* vp = vbase + at;
             if (kC == 8) {                              // lane = (token half, group)
                 const int off = (lane & 15) * kTokenBlock + 8 * (lane >> 4);
-                const uint2 a = *reinterpret_cast<const uint2*>(kp + off), b = *reinterpret_cast<const uint2*>(vp + off);
-                kw[0] = a.x; kw[1] = a.y; vw[0] = b.x; vw[1] = b.y;
+                const uint2 a = *reinterpret_cast<const uint2*>(kp + off);
+                kw[0] = a.x; kw[1] = a.y;
+                if (kSums) {
+                    const uint2 b = *reinterpret_cast<const uint2*>(vp + off);
+                    vw[0] = b.x; vw[1] = b.y;
+                }
             } else if (kC == 4) {                       // lane = group
-                const uint4 a = *reinterpret_cast<const uint4*>(kp + lane * kTokenBlock), b = *reinterpret_cast<const uint4*>(vp + lane * kTokenBlock);
+                const uint4 a = *reinterpret_cast<const uint4*>(kp + lane * kTokenBlock);
                 kw[0] = a.x; kw[1] = a.y; kw[2 % kW] = a.z; kw[3 % kW] = a.w;
-                vw[0] = b.x; vw[1] = b.y; vw[2 % kW] = b.z; vw[3 % kW] = b.w;
+                if (kSums) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(vp + lane * kTokenBlock);
+                    vw[0] = b.x; vw[1] = b.y; vw[2 % kW] = b.z; vw[3 % kW] = b.w;
+                }
             } else {                                    // lane = (token half, chunk of four groups, taken in another order by the other half)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int off = (4 * (lane & 15) + (i ^ (lane >> 4))) * kTokenBlock + 8 * (lane >> 4);
-                    const uint2 a = *reinterpret_cast<const uint2*>(kp + off), b = *reinterpret_cast<const uint2*>(vp + off);
-                    kw[(2 * i) % kW] = a.x; kw[(2 * i + 1) % kW] = a.y; vw[(2 * i) % kW] = b.x; vw[(2 * i + 1) % kW] = b.y;
+                    const uint2 a = *reinterpret_cast<const uint2*>(kp + off);
+                    kw[(2 * i) % kW] = a.x; kw[(2 * i + 1) % kW] = a.y;
+                    if (kSums) {
+                        const uint2 b = *reinterpret_cast<const uint2*>(vp + off);
+                        vw[(2 * i) % kW] = b.x; vw[(2 * i + 1) % kW] = b.y;
+                    }
                 }
             }
         };
@@ -506,7 +529,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             if (!__all_sync(0xffffffffu, ok)) break;
             if (kBounded && lane == 0) ctl->hole[stage][pw] = hole;
             fill(kw, C::kKcbOffset, C::kKtOffset + stage * C::kTileBytes);
-            fill(vw, C::kVcbOffset, C::kVtOffset + stage * C::kTileBytes);
+            if (kSums) fill(vw, C::kVcbOffset, C::kVtOffset + stage * C::kTileBytes);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) pf_arrive(&ctl->full[stage]);
@@ -539,6 +562,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                             pf_mma(tm + C::kSCol, tm + C::kQCol + 64 * t + 8 * ks,
                                    kdesc + (stage * C::kTileBytes + (ks >> 2) * C::kHalfBytes + (ks & 3) * 32) / 16, kScores, ks > 0);
                         pf_commit(&ctl->s_full[t]);
+                        if (!kSums && t == kHalves - 1) pf_commit(&ctl->empty[stage]);
                     }
                 }
             }
@@ -549,7 +573,31 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             __syncwarp();
             pf_drain(&ctl->drained[0]);
         }
-    } else if (warp == C::kSumWarp) {
+    } else if (!kSums && warp == C::kSumWarp) {
+        // ---------------------------------------------------------------- masses: the row tiles' and warps' sums to one, two tokens per lane
+        if constexpr (kWhat == kPfMass) {
+            const volatile float* sums = reinterpret_cast<const float*>(smem + C::kVtOffset);
+            const int64_t row_tile = bounded.row_tiles > 1 ? tile : 0;
+            const int64_t base = ((row_tile * sh.n_seq + s) * sh.n_kv_heads + hkv) * sh.max_tokens;
+            const bool old = bounded.mass_in && bounded.row_tiles == 1;
+            for (int jt = 0; jt < n_tiles; ++jt) {
+                const int64_t t0 = (int64_t)tile_at(jt) * C::kTile + lane;
+                float sum[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) sum[k] = old && t0 + 32 * k < n ? bounded.mass_in[base + t0 + 32 * k] : 0.f;
+                if (!__all_sync(0xffffffffu, pf_wait(ctl, &ctl->p_full[lane % n_halves], (uint32_t)jt & 1u))) break;
+                float add[2] = {0.f, 0.f};
+                for (int i = 0; i < 4 * n_halves; ++i)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) add[k] += sums[((jt & 1) * 8 + i) * C::kTile + 32 * k + lane];
+                __syncwarp();
+                if (lane == 0) pf_arrive(&ctl->pv_done[0]);                 // the next ones may come
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (t0 + 32 * k < n) bounded.mass_out[base + t0 + 32 * k] = sum[k] + add[k];
+            }
+        }
+    } else if (kSums && warp == C::kSumWarp) {
         // ---------------------------------------------------------------- sums: P Vhat, in the same order
         constexpr uint32_t kSums = (1u << 4) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);   // N = 128, B's rows along N
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), vdesc = pf_desc_lo(smem_u32(smem + C::kVtOffset), C::kHalfBytes);
@@ -614,6 +662,16 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             }
             float m = -INFINITY, l = 0.f;                                   // reference of the weights (log2 domain), the sum of this thread's
             bool ok = true;
+            if constexpr (kWhat == kPfMass) {                               // the row's log-sum-exp, from the parts of its context
+                const float* of = bounded.partials + ((int64_t)(blockIdx.x / bounded.parts) * bounded.parts * C::kRows + rho) * 2;
+                for (int i = 0; i < bounded.parts; ++i) m = fmaxf(m, of[(int64_t)i * C::kRows * 2]);
+                for (int i = 0; i < bounded.parts; ++i) {
+                    const float mi = of[(int64_t)i * C::kRows * 2];
+                    if (mi != -INFINITY) l += exp2f(mi - m) * of[(int64_t)i * C::kRows * 2 + 1];
+                }
+                // (a row that sees nothing: no weight; a row that is none: none of its scores, which are zero, counts)
+                m = !(qi < n_q && rho < rows_used) ? INFINITY : l == 0.f ? 0.f : m + log2f(l);
+            }
 #pragma unroll 1
             for (int jt = 0; jt < n_tiles; ++jt) {
                 ok &= pf_wait(ctl, &ctl->s_full[t], (uint32_t)jt & 1u);
@@ -646,6 +704,24 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                     for (int i = 0; i < 32; ++i)
                         if (!((sees >> i) & 1u)) sa[i] = -INFINITY;
                 }
+                if constexpr (kWhat == kPfMass) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sa[i] = ex2_approx(fmaf(sa[i], scale, -m));
+                    // lane i ends up with the sum of column i over the rows of the warp: with every step half of the columns changes hands
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                        for (int i = 0; i < o; ++i) {
+                            const float keep = lane & o ? sa[i + o] : sa[i], give = lane & o ? sa[i] : sa[i + o];
+                            sa[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                        }
+                    // (two places in turn: what lay here was taken before the last tile's sums were handed over)
+                    reinterpret_cast<volatile float*>(smem + C::kVtOffset)[((jt & 1) * 8 + t * 4 + (warp & 3)) * C::kTile + 32 * part + lane] =
+                        ok ? sa[0] : __int_as_float(0x7fffffff);
+                    if (jt > 0) ok &= pf_wait(ctl, &ctl->pv_done[0], (uint32_t)(jt - 1) & 1u);      // the last tile's have been taken
+                    __syncwarp();
+                    if (lane == 0) pf_arrive(&ctl->p_full[t]);
+                } else {
                 float mx[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mx[k] = max3(sa[k], sa[k + 4], sa[k + 8]);
@@ -656,6 +732,18 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], sa[28 + k]);
                 const float m_tile = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * scale;      // (-inf: the row sees nothing of this part)
+                if constexpr (kWhat == kPfLse) {
+                    const float m_new = fmaxf(m, m_tile), mm = m_new == -INFINITY ? 0.f : m_new;
+                    l *= m == -INFINITY ? 0.f : exp2f(m - mm);
+                    m = m_new;
+                    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        l0 += ex2_approx(fmaf(sa[2 * i], scale, -mm));
+                        l1 += ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
+                    }
+                    l += l0 + l1;
+                } else {
                 // The reference follows the maximum only when it is more than 8 (a factor of 256) behind: the sums rarely have to be
                 // rescaled, and fp16 weights up to 256 are as precise as weights up to 1.
                 const bool rescale = pf_pair_any(pair, m_tile > m + 8.f || (m == -INFINITY && m_tile > -INFINITY));
@@ -700,7 +788,25 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 pf_fence_before();
                 __syncwarp();
                 if (lane == 0) pf_arrive(&ctl->p_full[t]);
+                }
+                }
             }
+            if constexpr (kWhat == kPfLse) {                                // the two threads of a row to one
+                exchange[part * C::kRows + rho] = m;
+                pf_pair_sync(pair);
+                const float other = exchange[(part ^ 1) * C::kRows + rho], top = fmaxf(m, other);
+                pf_pair_sync(pair);
+                exchange[part * C::kRows + rho] = l = m == -INFINITY ? 0.f : l * exp2f(m - top);
+                pf_pair_sync(pair);
+                if (part == 0) {
+                    float* of = bounded.partials + ((int64_t)blockIdx.x * C::kRows + rho) * 2;
+                    of[0] = top;
+                    of[1] = ok ? l + exchange[C::kRows + rho] : __int_as_float(0x7fffffff);
+                }
+                pf_fence_before();
+            }
+            if constexpr (kWhat == kPfMass) pf_fence_before();
+            if constexpr (kWhat == kPfAttn) {
             exchange[part * C::kRows + rho] = l;
             pf_pair_sync(pair);
             l += exchange[(part ^ 1) * C::kRows + rho];
@@ -750,6 +856,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 __syncwarp();
             }
             pf_fence_before();
+            }
         }
     } else if (warp < 4 * n_halves) {
         // ---------------------------------------------------------------- softmax: a thread per row

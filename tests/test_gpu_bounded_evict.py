@@ -9,7 +9,7 @@ from tests import bounded as B
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 SCALE = 128 ** -0.5
-VARIANTS = [1, 2]
+VARIANTS = [0, 1, 2, 3]
 
 
 def mass_tolerance(case, s, q, n, p):
@@ -23,7 +23,7 @@ def mass_tolerance(case, s, q, n, p):
 
 
 @pytest.mark.parametrize("variant", VARIANTS)
-@pytest.mark.parametrize("c,Hq,Hkv,n_q", [(8, 8, 2, 1), (4, 4, 4, 1), (2, 6, 2, 5), (8, 8, 1, 32), (8, 20, 1, 3), (4, 3, 3, 70)])
+@pytest.mark.parametrize("c,Hq,Hkv,n_q", [(8, 8, 2, 1), (4, 4, 4, 1), (2, 6, 2, 5), (8, 8, 1, 32), (8, 20, 1, 3), (4, 3, 3, 70), (8, 4, 1, 150), (2, 6, 2, 200)])
 def test_mass(variant, c, Hq, Hkv, n_q):
     lens = [700, n_q, 1, 0, 333, 64 + n_q]
     cap = 709
@@ -70,9 +70,10 @@ def test_mass_of_long_contexts_and_many_sequences(variant):
             assert ((got[s, :, :n].double() - p.view(2, -1, n).sum(1)).abs() <= mass_tolerance(case, s, q[s], n, p)).all(), s
 
 
-def test_mass_repeats_bit_by_bit():
+@pytest.mark.parametrize("n_q", [1, 3, 70, 300])
+def test_mass_repeats_bit_by_bit(n_q):
     case = B.Case(9, 8, 8, 8, 2, [5000, 700], 5008)
-    q = case.queries(2, 3)
+    q = case.queries(2, n_q)
     k, _ = case.contiguous()
     first = cq.cq_attn_mass(q, k, case.kcb, case.seq_lens(), SCALE, 8, 8, 5008)
     for _ in range(3):

@@ -71,8 +71,8 @@ __global__ void __launch_bounds__(kWarps * 32) bounded_plain_kernel(BoundedArgs 
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
         dot *= a.scale_log2e;
-        const float m_new = fmaxf(m, dot);
-        const float corr = exp2f(m - m_new), p = exp2f(dot - m_new);
+        const float m_new = fmaxf(m, dot), ref = m_new == -INFINITY ? 0.f : m_new;      // (a score that is no number moves no reference)
+        const float corr = exp2f(m - ref), p = exp2f(dot - ref);
         l = l * corr + p;
 #pragma unroll
         for (int j = 0; j < kLaneCh; ++j) acc[j] = fmaf(p, vv[j], acc[j] * corr);
@@ -84,12 +84,12 @@ __global__ void __launch_bounds__(kWarps * 32) bounded_plain_kernel(BoundedArgs 
     __syncthreads();
     float M = -INFINITY, L = 0.f;
     for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red_m[w]);
-    for (int w = 0; w < kWarps; ++w) L += red_m[w] == -INFINITY ? 0.f : exp2f(red_m[w] - M) * red_l[w];
+    auto bring = [&](int w) { return red_m[w] == -INFINITY ? 1.f : exp2f(red_m[w] - M); };      // (no reference: the sums are zero, or no numbers)
+    for (int w = 0; w < kWarps; ++w) L += bring(w) * red_l[w];
     for (int d = threadIdx.x; d < sh.head_dim; d += blockDim.x) {
         float x = 0.f;
-        for (int w = 0; w < kWarps; ++w)
-            if (red_m[w] != -INFINITY) x = fmaf(exp2f(red_m[w] - M), red_acc[w][d], x);
-        a.out[row * sh.head_dim + d] = __float2half_rn(L > 0.f ? x / L : 0.f);       // nothing seen: a zero row
+        for (int w = 0; w < kWarps; ++w) x = fmaf(bring(w), red_acc[w][d], x);
+        a.out[row * sh.head_dim + d] = __float2half_rn(L == 0.f ? 0.f : x / L);      // nothing seen: a zero row
     }
 }
 
@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(kWarps * 32) mass_lse_kernel(BoundedArgs a, fl
     float m = -INFINITY, l = 0.f;
     for (int t = warp; t <= pos; t += kWarps) {
         const float x = plain_score(a, kcb, a.kc + block_offset(a, s, hkv, t / kTokenBlock), qd, t % kTokenBlock);
-        const float m_new = fmaxf(m, x);
-        l = l * exp2f(m - m_new) + exp2f(x - m_new);
+        const float m_new = fmaxf(m, x), ref = m_new == -INFINITY ? 0.f : m_new;
+        l = l * exp2f(m - ref) + exp2f(x - ref);
         m = m_new;
     }
     if (lane == 0) { red_m[warp] = m; red_l[warp] = l; }
@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(kWarps * 32) mass_lse_kernel(BoundedArgs a, fl
     if (threadIdx.x == 0) {
         float M = -INFINITY, L = 0.f;
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red_m[w]);
-        for (int w = 0; w < kWarps; ++w) L += red_m[w] == -INFINITY ? 0.f : exp2f(red_m[w] - M) * red_l[w];
-        lse[row] = L > 0.f ? M + log2f(L) : -INFINITY;
+        for (int w = 0; w < kWarps; ++w) L += (red_m[w] == -INFINITY ? 1.f : exp2f(red_m[w] - M)) * red_l[w];
+        lse[row] = L == 0.f ? -INFINITY : M + log2f(L);
     }
 }
 

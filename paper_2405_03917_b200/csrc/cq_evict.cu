@@ -8,9 +8,12 @@
 //       then ranked against each other, and the positions that stay are listed in order (ballots in a warp, one scan over the warps).
 //       Masses crowd in few bins: every lane counts in a column of its own, so that the lanes of a warp never meet.  What bounds it is
 //       the number of instructions per token: 32 sequences x 40 heads of 8192 ... 32768 tokens: 345 us with a shared column per bin
-//       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, see below for now.
+//       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, 161 us now (105 MB of
+//       masses: 16 us).
 //   evict_move_kernel    a warp per 16 tokens that stay: a lane takes one (tensor, group) of them, a byte load per token (the
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
+//       187 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
+//       nearly all codes are read (176 us with what is written, at the copy rate).
 //       In place a CTA goes through its (sequence, head) in order: positions only ever move down, and all reads of a turn are done
 //       before its writes.
 #include "cq_bounded.cuh"

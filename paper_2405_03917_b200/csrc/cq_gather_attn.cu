@@ -615,43 +615,43 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
                     for (int j = 0; j < kSc; ++j)
                         if (t0 + j < it.n) sums[t0 + j] = was[j] + (broken ? __int_as_float(0x7fffffff) : w[j]);
             } else {
-            float top = fmaxf(sc[0], sc[1]);
-            if (kSc == 4) top = fmaxf(top, fmaxf(sc[2 % kSc], sc[3 % kSc]));
-            top *= scale;
-            if (__any_sync(0xffffffffu, top > m_ref + 8.f)) {
+                float top = fmaxf(sc[0], sc[1]);
+                if (kSc == 4) top = fmaxf(top, fmaxf(sc[2 % kSc], sc[3 % kSc]));
+                top *= scale;
+                if (__any_sync(0xffffffffu, top > m_ref + 8.f)) {
 #pragma unroll
-                for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float m_new = fmaxf(m_ref, top);
-                float f = m_ref == -INFINITY ? 0.f : ex2f(m_ref - m_new);
-                m_ref = m_new;
-                l *= f;
-                if constexpr (kMode == kAttn) {
-                    if (kRows == 4) f = __shfl_sync(0xffffffffu, f, r & 3); // (the accumulators are row r & 3's)
+                    for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const float m_new = fmaxf(m_ref, top);
+                    float f = m_ref == -INFINITY ? 0.f : ex2f(m_ref - m_new);
+                    m_ref = m_new;
+                    l *= f;
+                    if constexpr (kMode == kAttn) {
+                        if (kRows == 4) f = __shfl_sync(0xffffffffu, f, r & 3); // (the accumulators are row r & 3's)
 #pragma unroll
-                    for (int i = 0; i < kNT; ++i)
+                        for (int i = 0; i < kNT; ++i)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[i][k] *= f;
+                            for (int k = 0; k < 4; ++k) acc[i][k] *= f;
+                    }
                 }
-            }
-            const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-            if constexpr (kMode == kLse) {
+                const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+                if constexpr (kMode == kLse) {
 #pragma unroll
-                for (int j = 0; j < kSc; ++j) l += ex2f(fmaf(sc[j], scale, -ref));
-                const int blk = block_of(it, turn);
-                if (kRows == 4 && scores && blk >= 0)
-                    *reinterpret_cast<float2*>(scores + (int64_t)blk * 64) = make_float2(sc[0] * scale, sc[1] * scale);
-            } else {
-            uint32_t y[kSc / 2];
+                    for (int j = 0; j < kSc; ++j) l += ex2f(fmaf(sc[j], scale, -ref));
+                    const int blk = block_of(it, turn);
+                    if (kRows == 4 && scores && blk >= 0)
+                        *reinterpret_cast<float2*>(scores + (int64_t)blk * 64) = make_float2(sc[0] * scale, sc[1] * scale);
+                } else {
+                    uint32_t y[kSc / 2];
 #pragma unroll
-            for (int j = 0; j < kSc / 2; ++j) {
-                const __half2 h = __floats2half2_rn(ex2f(fmaf(sc[2 * j], scale, -ref)), ex2f(fmaf(sc[2 * j + 1], scale, -ref)));
-                const float2 f = __half22float2(h);                         // (the normaliser sums the weights as they are used)
-                l += f.x + f.y;
-                y[j] = *reinterpret_cast<const uint32_t*>(&h);
-            }
+                    for (int j = 0; j < kSc / 2; ++j) {
+                        const __half2 h = __floats2half2_rn(ex2f(fmaf(sc[2 * j], scale, -ref)), ex2f(fmaf(sc[2 * j + 1], scale, -ref)));
+                        const float2 f = __half22float2(h);                         // (the normaliser sums the weights as they are used)
+                        l += f.x + f.y;
+                        y[j] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
 #pragma unroll
-            for (int i = 0; i < kX; ++i) x[i] = kRows == 4 ? __shfl_sync(0xffffffffu, y[0], (2 * (p & 2) + i) * 4 + (r & 3)) : y[i % (kSc / 2)];
-            }
+                    for (int i = 0; i < kX; ++i) x[i] = kRows == 4 ? __shfl_sync(0xffffffffu, y[0], (2 * (p & 2) + i) * 4 + (r & 3)) : y[i % (kSc / 2)];
+                }
             }
         };
         // Four rows: row r & 3, tokens 8 (p / 2) + {0 ... 7}; eight: row r, tokens 4 p + {0 ... 3}
@@ -724,75 +724,75 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
             copies_wait_all();
             __syncthreads();
         } else {
-        // ---- the warps' sums to one
-        // Every warp brings its accumulators to the largest reference; then they are plain sums.
+            // ---- the warps' sums to one
+            // Every warp brings its accumulators to the largest reference; then they are plain sums.
 #pragma unroll
-        for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        const bool speaks = kRows == 4 ? r == 0 : p == 0;                   // for its row
-        if (speaks) wm[warp * 8 + my_row] = m_ref;
-        __syncthreads();
-        if (more_next) copy_queries(next);                                  // (this item's have been read)
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w * 8 + my_row]);
-        float bring = m_ref == -INFINITY ? 0.f : ex2f(m_ref - M);
-        if (speaks) wl[warp * 8 + my_row] = l * bring;
-        if (kRows == 4) bring = __shfl_sync(0xffffffffu, bring, r & 3);
-        const bool whole = it.begins && it.ends;
-        float* part = partials + (int64_t)(2 * blockIdx.x + (it.begins ? 1 : 0)) * partial_floats(kRows, kMode);
-        if constexpr (kMode == kLse) {
+            for (int o = kRows == 4 ? 4 : 1; o <= (kRows == 4 ? 16 : 2); o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            const bool speaks = kRows == 4 ? r == 0 : p == 0;                   // for its row
+            if (speaks) wm[warp * 8 + my_row] = m_ref;
             __syncthreads();
-            if (threadIdx.x < kRows) {                                      // (the first lane of a row's lanes holds the largest reference)
-                float L = 0.f, top = -INFINITY;
+            if (more_next) copy_queries(next);                                  // (this item's have been read)
+            float M = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    L += wl[w * 8 + threadIdx.x];
-                    top = fmaxf(top, wm[w * 8 + threadIdx.x]);
-                }
-                if (broken) L = __int_as_float(0x7fffffff);
-                if (!whole) {
-                    part[threadIdx.x] = top;
-                    part[kRows + threadIdx.x] = L;
-                } else if ((int)threadIdx.x < it.rows) {
-                    mass.lse[((int64_t)it.seq * sh.n_kv_heads + it.head) * mass.row_stride + it.row0 + threadIdx.x] = top + log2f(L);
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w * 8 + my_row]);
+            float bring = m_ref == -INFINITY ? 0.f : ex2f(m_ref - M);
+            if (speaks) wl[warp * 8 + my_row] = l * bring;
+            if (kRows == 4) bring = __shfl_sync(0xffffffffu, bring, r & 3);
+            const bool whole = it.begins && it.ends;
+            float* part = partials + (int64_t)(2 * blockIdx.x + (it.begins ? 1 : 0)) * partial_floats(kRows, kMode);
+            if constexpr (kMode == kLse) {
+                __syncthreads();
+                if (threadIdx.x < kRows) {                                      // (the first lane of a row's lanes holds the largest reference)
+                    float L = 0.f, top = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        L += wl[w * 8 + threadIdx.x];
+                        top = fmaxf(top, wm[w * 8 + threadIdx.x]);
+                    }
+                    if (broken) L = __int_as_float(0x7fffffff);
+                    if (!whole) {
+                        part[threadIdx.x] = top;
+                        part[kRows + threadIdx.x] = L;
+                    } else if ((int)threadIdx.x < it.rows) {
+                        mass.lse[((int64_t)it.seq * sh.n_kv_heads + it.head) * mass.row_stride + it.row0 + threadIdx.x] = top + log2f(L);
+                    }
                 }
             }
-        }
-        if constexpr (kMode == kAttn) {
-        float* mine = reinterpret_cast<float*>(stage0);
+            if constexpr (kMode == kAttn) {
+                float* mine = reinterpret_cast<float*>(stage0);
 #pragma unroll
-        for (int i = 0; i < kNT * 4; ++i) mine[i * 32 + lane] = acc[i >> 2][i & 3] * bring;
-        __syncthreads();
+                for (int i = 0; i < kNT * 4; ++i) mine[i * 32 + lane] = acc[i >> 2][i & 3] * bring;
+                __syncthreads();
 #pragma unroll 2
-        for (int reg = warp; reg < kNT * 4; reg += kWarps) {                // this warp sums one register of all warps, lane by lane
-            int row, channel;
-            place_of<kC, kRows>(reg, lane, row, channel);
-            float L = 0.f, sum_of = 0.f;
+                for (int reg = warp; reg < kNT * 4; reg += kWarps) {                // this warp sums one register of all warps, lane by lane
+                    int row, channel;
+                    place_of<kC, kRows>(reg, lane, row, channel);
+                    float L = 0.f, sum_of = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                L += wl[w * 8 + row];
-                sum_of += reinterpret_cast<const float*>(smem + C::kStageOffset + w * kWarpBytes)[reg * 32 + lane];
-            }
-            if (broken) sum_of = __int_as_float(0x7fffffff);                // (nothing that could be taken for a result)
-            if (whole) {
-                if (row < it.rows) {
-                    const int at = it.row0 + row;
-                    a.out[(((int64_t)it.q_first + at / R) * sh.n_q_heads + it.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum_of / L : sum_of);
+                    for (int w = 0; w < kWarps; ++w) {
+                        L += wl[w * 8 + row];
+                        sum_of += reinterpret_cast<const float*>(smem + C::kStageOffset + w * kWarpBytes)[reg * 32 + lane];
+                    }
+                    if (broken) sum_of = __int_as_float(0x7fffffff);                // (nothing that could be taken for a result)
+                    if (whole) {
+                        if (row < it.rows) {
+                            const int at = it.row0 + row;
+                            a.out[(((int64_t)it.q_first + at / R) * sh.n_q_heads + it.head * R + at % R) * 128 + channel] = __float2half_rn(L == 0.f ? sum_of : sum_of / L);
+                        }
+                    } else {
+                        part[2 * kRows + reg * 32 + lane] = sum_of;
+                        if (reg == 0 && p == 0 && r < kRows) part[kRows + row] = L;
+                    }
                 }
-            } else {
-                part[2 * kRows + reg * 32 + lane] = sum_of;
-                if (reg == 0 && p == 0 && r < kRows) part[kRows + row] = L;
+                if (!whole && warp == 0 && speaks) part[my_row] = M;
             }
-        }
-        if (!whole && warp == 0 && speaks) part[my_row] = M;
-        }
-        copies_wait_all();
-        __syncthreads();
-        if (!whole && threadIdx.x == 0) {
-            Cut c;
-            c.head = it.head; c.seq = it.seq; c.tile = it.tile; c.state = it.ends ? 2 : 1;
-            cuts[2 * blockIdx.x + (it.begins ? 1 : 0)] = c;
-        }
+            copies_wait_all();
+            __syncthreads();
+            if (!whole && threadIdx.x == 0) {
+                Cut c;
+                c.head = it.head; c.seq = it.seq; c.tile = it.tile; c.state = it.ends ? 2 : 1;
+                cuts[2 * blockIdx.x + (it.begins ? 1 : 0)] = c;
+            }
         }
         it = next;
         where = where_next;
@@ -829,23 +829,23 @@ gather_merge_kernel(BoundedArgs a, MassArgs mass, const float* __restrict__ part
         for (int j = k; j <= last; ++j) L = fmaf(part(j)[0] == -INFINITY ? 0.f : ex2f(part(j)[0] - M), part(j)[kRows], L);
         mass.lse[((int64_t)first.seq * a.sh.n_kv_heads + first.head) * mass.row_stride + row0 + lane] = M + log2f(L);
     } else {
-    for (int reg = warp; reg < (kRows == 4 ? 16 : 32); reg += 16) {
-        int row, channel;
-        place_of<kC, kRows>(reg, lane, row, channel);
-        auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows, kMode); };
-        float M = -INFINITY, L = 0.f, sum = 0.f;
+        for (int reg = warp; reg < (kRows == 4 ? 16 : 32); reg += 16) {
+            int row, channel;
+            place_of<kC, kRows>(reg, lane, row, channel);
+            auto part = [&](int j) { return partials + (int64_t)(2 * j + (j == k)) * partial_floats(kRows, kMode); };
+            float M = -INFINITY, L = 0.f, sum = 0.f;
 #pragma unroll 4
-        for (int j = k; j <= last; ++j) M = fmaxf(M, part(j)[row]);
+            for (int j = k; j <= last; ++j) M = fmaxf(M, part(j)[row]);
 #pragma unroll 4
-        for (int j = k; j <= last; ++j) {
-            const float mj = part(j)[row], f = mj == -INFINITY ? 0.f : ex2f(mj - M);
-            L = fmaf(f, part(j)[kRows + row], L);
-            sum = fmaf(f, part(j)[2 * kRows + reg * 32 + lane], sum);
+            for (int j = k; j <= last; ++j) {
+                const float mj = part(j)[row], f = mj == -INFINITY ? 0.f : ex2f(mj - M);
+                L = fmaf(f, part(j)[kRows + row], L);
+                sum = fmaf(f, part(j)[2 * kRows + reg * 32 + lane], sum);
+            }
+            const int at = row0 + row;
+            if (at < sv.m * R)
+                a.out[(((int64_t)sv.row0 + at / R) * a.sh.n_q_heads + first.head * R + at % R) * 128 + channel] = __float2half_rn(L == 0.f ? sum : sum / L);
         }
-        const int at = row0 + row;
-        if (at < sv.m * R)
-            a.out[(((int64_t)sv.row0 + at / R) * a.sh.n_q_heads + first.head * R + at % R) * 128 + channel] = __float2half_rn(L > 0.f ? sum / L : sum);
-    }
     }
 }
 

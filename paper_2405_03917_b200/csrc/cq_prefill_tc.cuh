@@ -58,6 +58,7 @@ struct PfCtl {
     uint32_t tmem_base;
     int failed;                           // a wait gave up
     alignas(4) uint8_t hole[PfCfg::kStages][4];      // bounded: the 16-token block of the stage lies in no page
+    int found, number;                    // bounded: this CTA's sequence and row tile
 };
 static_assert(sizeof(PfCtl) <= 256, "control block");
 
@@ -199,9 +200,43 @@ __device__ __forceinline__ int pf_tiles_of(const BoundedArgs& a, const SeqView& 
     return rows < a.least_rows || rows > a.most_rows ? 0 : (v.m + q_per_tile - 1) / q_per_tile;
 }
 // The sequence that row tile `index` of all belongs to (-1: none) and its number there.  Entered by whole warps; the same in all lanes.
+// With as many new tokens in every sequence: a division.  Otherwise up to kPfSorted sequences are taken in the order of their lengths,
+// the longest first (a row tile of a long one started last would keep its SM busy alone: 24 sequences of 600 to 9001 tokens with 1 to
+// 512 new ones, 307 us, in their own order 395); of more than that, whose row tiles fill the GPU many times over, the counts alone are
+// looked at, for the comparison takes a CTA some ten cycles per sequence (2 us at 64).
+constexpr int kPfSorted = 64;
 __device__ __forceinline__ int pf_find_tile(const BoundedArgs& a, int index, int q_per_tile, int& tile)
 {
     const int lane = threadIdx.x & 31, n_seq = (int)a.sh.n_seq;
+    if (!a.q_offsets) {
+        const int each = (a.max_q + q_per_tile - 1) / q_per_tile;
+        tile = index % each;
+        return index / each < n_seq ? index / each : -1;
+    }
+    if (n_seq <= kPfSorted) {
+        int len[2], tiles[2], before[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const SeqView v = seq_view(a, lane + 32 * k < n_seq ? lane + 32 * k : 0);
+            len[k] = v.n;
+            tiles[k] = lane + 32 * k < n_seq ? pf_tiles_of(a, v, q_per_tile) : 0;
+        }
+        for (int j = 0; j < n_seq; ++j) {
+            const int len_j = __shfl_sync(0xffffffffu, j < 32 ? len[0] : len[1], j & 31);
+            const int tiles_j = __shfl_sync(0xffffffffu, j < 32 ? tiles[0] : tiles[1], j & 31);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) before[k] += len_j > len[k] || (len_j == len[k] && j < lane + 32 * k) ? tiles_j : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t hit = __ballot_sync(0xffffffffu, index >= before[k] && index < before[k] + tiles[k]);
+            if (hit) {
+                tile = index - __shfl_sync(0xffffffffu, before[k], __ffs(hit) - 1);
+                return 32 * k + __ffs(hit) - 1;
+            }
+        }
+        return -1;
+    }
     for (int s0 = 0; s0 < n_seq; s0 += 32) {
         const int mine = s0 + lane < n_seq ? pf_tiles_of(a, seq_view(a, s0 + lane), q_per_tile) : 0;
         int incl = mine;
@@ -255,8 +290,13 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
     if constexpr (kBounded) {
         const int item = blockIdx.x / bounded.parts;
         hkv = item % sh.n_kv_heads;
-        int number = 0;
-        const int found = pf_find_tile(bounded.a, item / sh.n_kv_heads, q_per_tile, number);
+        if (warp == 0) {
+            int number = 0;
+            ctl->found = pf_find_tile(bounded.a, item / sh.n_kv_heads, q_per_tile, number);      // (all lanes the same)
+            ctl->number = number;
+        }
+        __syncthreads();
+        const int found = ctl->found, number = ctl->number;
         if (found < 0) return;
         const SeqView sv = seq_view(bounded.a, found);
         s = found;
@@ -667,7 +707,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 for (int i = 0; i < bounded.parts; ++i) m = fmaxf(m, of[(int64_t)i * C::kRows * 2]);
                 for (int i = 0; i < bounded.parts; ++i) {
                     const float mi = of[(int64_t)i * C::kRows * 2];
-                    if (mi != -INFINITY) l += exp2f(mi - m) * of[(int64_t)i * C::kRows * 2 + 1];
+                    l += (mi == -INFINITY ? 1.f : exp2f(mi - m)) * of[(int64_t)i * C::kRows * 2 + 1];      // (no reference: zero, or no number)
                 }
                 // (a row that sees nothing: no weight; a row that is none: none of its scores, which are zero, counts)
                 m = !(qi < n_q && rho < rows_used) ? INFINITY : l == 0.f ? 0.f : m + log2f(l);
@@ -722,73 +762,73 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                     __syncwarp();
                     if (lane == 0) pf_arrive(&ctl->p_full[t]);
                 } else {
-                float mx[4];
+                    float mx[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = max3(sa[k], sa[k + 4], sa[k + 8]);
+                    for (int k = 0; k < 4; ++k) mx[k] = max3(sa[k], sa[k + 4], sa[k + 8]);
 #pragma unroll
-                for (int i = 12; i < 28; i += 8)
+                    for (int i = 12; i < 28; i += 8)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], sa[i + k], sa[i + 4 + k]);
+                        for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], sa[i + k], sa[i + 4 + k]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], sa[28 + k]);
-                const float m_tile = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * scale;      // (-inf: the row sees nothing of this part)
-                if constexpr (kWhat == kPfLse) {
-                    const float m_new = fmaxf(m, m_tile), mm = m_new == -INFINITY ? 0.f : m_new;
-                    l *= m == -INFINITY ? 0.f : exp2f(m - mm);
-                    m = m_new;
-                    float l0 = 0.f, l1 = 0.f;
+                    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], sa[28 + k]);
+                    const float m_tile = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * scale;      // (-inf: the row sees nothing of this part)
+                    if constexpr (kWhat == kPfLse) {
+                        const float m_new = fmaxf(m, m_tile), mm = m_new == -INFINITY ? 0.f : m_new;
+                        l *= m == -INFINITY ? 0.f : exp2f(m - mm);
+                        m = m_new;
+                        float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        l0 += ex2_approx(fmaf(sa[2 * i], scale, -mm));
-                        l1 += ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
-                    }
-                    l += l0 + l1;
-                } else {
-                // The reference follows the maximum only when it is more than 8 (a factor of 256) behind: the sums rarely have to be
-                // rescaled, and fp16 weights up to 256 are as precise as weights up to 1.
-                const bool rescale = pf_pair_any(pair, m_tile > m + 8.f || (m == -INFINITY && m_tile > -INFINITY));
-                float f = 1.f;
-                if (rescale) {
-                    exchange[part * C::kRows + rho] = m_tile;
-                    pf_pair_sync(pair);
-                    const float m_new = max3(m, m_tile, exchange[(part ^ 1) * C::kRows + rho]);
-                    pf_pair_sync(pair);
-                    f = m == -INFINITY ? 0.f : exp2f(m - m_new);
-                    m = m_new;
-                    l *= f;
-                }
-                const float mm = m == -INFINITY ? 0.f : m;
-                uint32_t p[16];
-                float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x0 = ex2_approx(fmaf(sa[2 * i], scale, -mm)), x1 = ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
-                    l0 += x0;
-                    l1 += x1;
-                    p[i] = pack_half2(x0, x1);
-                }
-                l += l0 + l1;
-                if (jt > 0) {                                               // the last sums are done with the weights' columns
-                    ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(jt - 1) & 1u);
-                    pf_fence_after();
-                    if (rescale) {
-#pragma unroll 1
-                        for (int c0 = 0; c0 < 64; c0 += 32) {
-                            uint32_t o[32];
-                            pf_ld32(o, o_addr + c0);
-                            pf_ld_wait(o);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            pf_st32(o_addr + c0, o);
+                        for (int i = 0; i < 16; ++i) {
+                            l0 += ex2_approx(fmaf(sa[2 * i], scale, -mm));
+                            l1 += ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
                         }
+                        l += l0 + l1;
+                    } else {
+                        // The reference follows the maximum only when it is more than 8 (a factor of 256) behind: the sums rarely have to be
+                        // rescaled, and fp16 weights up to 256 are as precise as weights up to 1.
+                        const bool rescale = pf_pair_any(pair, m_tile > m + 8.f || (m == -INFINITY && m_tile > -INFINITY));
+                        float f = 1.f;
+                        if (rescale) {
+                            exchange[part * C::kRows + rho] = m_tile;
+                            pf_pair_sync(pair);
+                            const float m_new = max3(m, m_tile, exchange[(part ^ 1) * C::kRows + rho]);
+                            pf_pair_sync(pair);
+                            f = m == -INFINITY ? 0.f : exp2f(m - m_new);
+                            m = m_new;
+                            l *= f;
+                        }
+                        const float mm = m == -INFINITY ? 0.f : m;
+                        uint32_t p[16];
+                        float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x0 = ex2_approx(fmaf(sa[2 * i], scale, -mm)), x1 = ex2_approx(fmaf(sa[2 * i + 1], scale, -mm));
+                            l0 += x0;
+                            l1 += x1;
+                            p[i] = pack_half2(x0, x1);
+                        }
+                        l += l0 + l1;
+                        if (jt > 0) {                                               // the last sums are done with the weights' columns
+                            ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(jt - 1) & 1u);
+                            pf_fence_after();
+                            if (rescale) {
+#pragma unroll 1
+                                for (int c0 = 0; c0 < 64; c0 += 32) {
+                                    uint32_t o[32];
+                                    pf_ld32(o, o_addr + c0);
+                                    pf_ld_wait(o);
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                    pf_st32(o_addr + c0, o);
+                                }
+                            }
+                        }
+                        pf_st16(p_addr, p);
+                        pf_st_wait();
+                        pf_fence_before();
+                        __syncwarp();
+                        if (lane == 0) pf_arrive(&ctl->p_full[t]);
                     }
-                }
-                pf_st16(p_addr, p);
-                pf_st_wait();
-                pf_fence_before();
-                __syncwarp();
-                if (lane == 0) pf_arrive(&ctl->p_full[t]);
-                }
                 }
             }
             if constexpr (kWhat == kPfLse) {                                // the two threads of a row to one
@@ -796,7 +836,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 pf_pair_sync(pair);
                 const float other = exchange[(part ^ 1) * C::kRows + rho], top = fmaxf(m, other);
                 pf_pair_sync(pair);
-                exchange[part * C::kRows + rho] = l = m == -INFINITY ? 0.f : l * exp2f(m - top);
+                exchange[part * C::kRows + rho] = l = m == -INFINITY ? l : l * exp2f(m - top);
                 pf_pair_sync(pair);
                 if (part == 0) {
                     float* of = bounded.partials + ((int64_t)blockIdx.x * C::kRows + rho) * 2;
@@ -807,55 +847,55 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             }
             if constexpr (kWhat == kPfMass) pf_fence_before();
             if constexpr (kWhat == kPfAttn) {
-            exchange[part * C::kRows + rho] = l;
-            pf_pair_sync(pair);
-            l += exchange[(part ^ 1) * C::kRows + rho];
-            // ---- normalise and write, through shared memory (the codebooks are done with when the last sums are), in whole lines
-            if (n_tiles > 0) ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(n_tiles - 1) & 1u);
-            ok = __all_sync(0xffffffffu, ok);
-            pf_fence_after();
-            const bool partial = bounded.parts > 1;                         // (partials: the accumulators as they are)
-            // nothing seen: a zero row; a wait gave up: NaN rows, so that nothing takes them for a result
-            const float inv = !ok ? __int_as_float(0x7fffffff) : partial ? 1.f : l > 0.f ? 1.f / l : 0.f;
-            float* to_part = nullptr;
-            if (partial) {
-                to_part = bounded.partials + ((int64_t)blockIdx.x * C::kRows + row0) * partial_stride(128);
-                if (part == 0) {
-                    to_part[lane * partial_stride(128)] = m;
-                    to_part[lane * partial_stride(128) + 1] = l;
-                }
-            }
-            uint8_t* block = smem + warp * 32 * C::kOutStride;
-#pragma unroll 1
-            for (int c0 = 0; c0 < 64; c0 += 32) {
-                uint32_t o[32];
-                if (n_tiles > 0) {
-                    pf_ld32(o, o_addr + c0);
-                    pf_ld_wait(o);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<float4*>(block + lane * C::kOutStride + 16 * i) =
-                        inv == 0.f || n_tiles == 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                   : make_float4(__uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
-                                                                 __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int rw = 4 * i + (lane >> 3), rr = row0 + rw, qr = qi0 + rr / R, column = 64 * part + c0 + 4 * (lane & 7);
-                    const float4 v = *reinterpret_cast<const float4*>(block + rw * C::kOutStride + 16 * (lane & 7));
-                    if (partial) {
-                        float* to = to_part + rw * partial_stride(128) + 2 + column;
-                        *reinterpret_cast<float2*>(to) = make_float2(v.x, v.y);
-                        *reinterpret_cast<float2*>(to + 2) = make_float2(v.z, v.w);
-                    } else if (qr < n_q && rr < rows_used) {
-                        *reinterpret_cast<uint2*>(bounded.a.out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + column) =
-                            make_uint2(pack_half2(v.x, v.y), pack_half2(v.z, v.w));
+                exchange[part * C::kRows + rho] = l;
+                pf_pair_sync(pair);
+                l += exchange[(part ^ 1) * C::kRows + rho];
+                // ---- normalise and write, through shared memory (the codebooks are done with when the last sums are), in whole lines
+                if (n_tiles > 0) ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(n_tiles - 1) & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                pf_fence_after();
+                const bool partial = bounded.parts > 1;                         // (partials: the accumulators as they are)
+                // nothing seen: a zero row; a wait gave up: NaN rows, so that nothing takes them for a result
+                const float inv = !ok ? __int_as_float(0x7fffffff) : partial ? 1.f : l == 0.f ? 0.f : 1.f / l;
+                float* to_part = nullptr;
+                if (partial) {
+                    to_part = bounded.partials + ((int64_t)blockIdx.x * C::kRows + row0) * partial_stride(128);
+                    if (part == 0) {
+                        to_part[lane * partial_stride(128)] = m;
+                        to_part[lane * partial_stride(128) + 1] = l;
                     }
                 }
-                __syncwarp();
-            }
-            pf_fence_before();
+                uint8_t* block = smem + warp * 32 * C::kOutStride;
+#pragma unroll 1
+                for (int c0 = 0; c0 < 64; c0 += 32) {
+                    uint32_t o[32];
+                    if (n_tiles > 0) {
+                        pf_ld32(o, o_addr + c0);
+                        pf_ld_wait(o);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<float4*>(block + lane * C::kOutStride + 16 * i) =
+                            inv == 0.f || n_tiles == 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                       : make_float4(__uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
+                                                                     __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int rw = 4 * i + (lane >> 3), rr = row0 + rw, qr = qi0 + rr / R, column = 64 * part + c0 + 4 * (lane & 7);
+                        const float4 v = *reinterpret_cast<const float4*>(block + rw * C::kOutStride + 16 * (lane & 7));
+                        if (partial) {
+                            float* to = to_part + rw * partial_stride(128) + 2 + column;
+                            *reinterpret_cast<float2*>(to) = make_float2(v.x, v.y);
+                            *reinterpret_cast<float2*>(to + 2) = make_float2(v.z, v.w);
+                        } else if (qr < n_q && rr < rows_used) {
+                            *reinterpret_cast<uint2*>(bounded.a.out + ((q_first + qr) * sh.n_q_heads + hkv * R + rr % R) * 128 + column) =
+                                make_uint2(pack_half2(v.x, v.y), pack_half2(v.z, v.w));
+                        }
+                    }
+                    __syncwarp();
+                }
+                pf_fence_before();
             }
         }
     } else if (warp < 4 * n_halves) {

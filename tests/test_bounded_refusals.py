@@ -125,3 +125,13 @@ def test_the_binding_names_what_is_wrong():
         cq.cq_window_attn(q, codes[:-1], codes, book, book, lens, 1.0, 8, 8, 256, 64)
     with pytest.raises(ValueError, match="come together"):
         cq.cq_evict(torch.zeros(2, 2, 256), codes, codes, lens, 128, 8, 8, 256, 16, k_codes_out=codes)
+
+
+@pytest.mark.parametrize("name", ["cq_window_attn_variant", "cq_paged_attn_variant", "cq_attn_mass_variant"])
+def test_kernels_that_a_caller_names(name):
+    call = caller(name, CALLS[name])
+    for variant in (2, 3):                                               # of shapes that are not theirs
+        for D, c, b in ((64, 8, 8), (128, 8, 10), (128, 16, 8), (256, 8, 8), (96, 3, 4)):
+            assert call(variant=variant, D=D, c=c, b=b) == UNSUPPORTED, (variant, D, c, b)
+    for variant in (-1, 4):
+        assert call(variant=variant) == SHAPE

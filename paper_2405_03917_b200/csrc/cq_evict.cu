@@ -14,6 +14,7 @@
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
 //       187 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
 //       nearly all codes are read (176 us with what is written, at the copy rate).
+//       (16-byte words of the source blocks instead, their bytes shifted in one by one: 268 us.)
 //       In place a CTA goes through its (sequence, head) in order: positions only ever move down, and all reads of a turn are done
 //       before its writes.
 #include "cq_bounded.cuh"
@@ -36,8 +37,11 @@ __device__ __forceinline__ uint32_t mass_key(float m)
 constexpr int kFewMost = 1024;                       // tokens that are ranked against each other
 
 // kEach: masses a thread keeps in registers (0: they are read again from memory for every pass)
+// Short contexts (kEach = 4) leave room for two CTAs on an SM: 32 x 32 heads of 500 ... 1000 tokens 39.5 -> 32.1 us, 64 x 32 76 -> 61 us, move
+// included.  (Longer ones with the upper halves of their keys in shared memory and two CTAs, so that registers suffice: 388 against 347 us for
+// the call above.  One kernel that selects and moves, two CTAs on an SM: 408 us.)
 template <int kEach>
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictArgs a)
+__global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_select_kernel(EvictArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

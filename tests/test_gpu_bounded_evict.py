@@ -222,3 +222,48 @@ def test_mass_with_less_workspace():
         for s, n in enumerate(case.lens):
             _, _, p = B.attend(case, s, q[s], n, SCALE)
             assert ((got[s, :, :n].double() - p.view(2, -1, n).sum(1)).abs() <= mass_tolerance(case, s, q[s], n, p)).all()
+
+
+# ------------------------------------------------------------------------------------------ more (sequence, head) pairs than two per SM
+
+MANY = dict(n_seq=50, H=6)
+
+
+@pytest.mark.parametrize("room", [None, 128])
+@pytest.mark.parametrize("c,b", [(8, 8), (2, 8), (8, 10), (128, 9)])
+@pytest.mark.parametrize("keep,sinks,recent", [(64, 4, 16), (100, 0, 100), (128, 5, 0)])
+def test_evict_of_many_heads(room, c, b, keep, sinks, recent):
+    g = np.random.default_rng(keep + c)
+    lens = [int(x) for x in g.integers(0, 300, MANY["n_seq"])]
+    lens[:4] = [keep, keep + 1, 0, 300]
+    case = B.Case(c + b + keep, c, b, MANY["H"], MANY["H"], lens, 304)
+    mass = g.exponential(1.0, (MANY["n_seq"], MANY["H"], 304)).astype(np.float32)
+    check_evict(case, mass, keep, sinks, recent, room)
+
+
+@pytest.mark.parametrize("room", [None, 512])
+def test_ties_and_values_that_are_no_numbers_of_many_heads(room):
+    g = np.random.default_rng(5)
+    n = MANY["n_seq"]
+    case = B.Case(15, 16, 8, MANY["H"], MANY["H"], [int(x) for x in g.integers(1, 2500, n)], 2512)
+    mass = g.exponential(1.0, (n, MANY["H"], 2512)).astype(np.float32)
+    mass[:10] = g.integers(0, 4, mass[:10].shape)                       # many alike: more than are ranked against each other
+    mass[10:14] = 0.0
+    mass[12, :, ::2] = -0.0
+    mass[14:18] = g.standard_normal(mass[14:18].shape)
+    mass[14, :, ::7], mass[15, :, 1::5], mass[16, :, 3::11] = np.inf, -np.inf, np.nan
+    mass[18] = -np.inf
+    mass.view(np.uint32)[19, :, ::13] = 0xffc00001                      # NaN of the other sign
+    bits = 0x3f800000 + np.stack([g.permutation(2512) for _ in range(10 * MANY["H"])]).reshape(10, MANY["H"], 2512)
+    mass[20:30] = bits.astype(np.uint32).view(np.float32)               # alike but for the last bits
+    check_evict(case, mass, 200, 4, 32, room)
+
+
+def test_many_heads_at_the_longest_capacities_of_a_kernel():
+    n = 38                                                              # x 8 heads = 304
+    for cap in (32768, 32769):
+        g = np.random.default_rng(cap)
+        lens = [cap, cap - 1, 5, 20000] + [int(x) for x in g.integers(0, 200, n - 4)]
+        case = B.Case(16, 128, 8, 8, 8, lens, cap)
+        mass = g.exponential(1.0, (n, 8, cap)).astype(np.float32)
+        check_evict(case, mass, 1000, 4, 100, 1008)

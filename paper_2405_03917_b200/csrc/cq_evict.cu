@@ -8,8 +8,8 @@
 //       then ranked against each other, and the positions that stay are listed in order (ballots in a warp, one scan over the warps).
 //       Masses crowd in few bins: every lane counts in a column of its own, so that the lanes of a warp never meet.  What bounds it is
 //       the number of instructions per token: 32 sequences x 40 heads of 8192 ... 32768 tokens: 345 us with a shared column per bin
-//       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, 161 us now (105 MB of
-//       masses: 16 us).
+//       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, 161 us with masses in
+//       registers, room for the longest, 120 us with a loop for each of three lengths (105 MB of masses: 16 us).
 //   evict_move_kernel    a warp per 16 tokens that stay: a lane takes one (tensor, group) of them, a byte load per token (the
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
 //       187 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
@@ -23,7 +23,6 @@ namespace cq {
 
 namespace {
 
-constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
 constexpr int kBins = 256;
 
 // Whole number of the same order as the mass, never zero: any NaN above all numbers (a sum with a NaN is the canonical one, which is
@@ -34,40 +33,28 @@ __device__ __forceinline__ uint32_t mass_key(float m)
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-constexpr int kFewMost = 1024;                       // tokens that are ranked against each other
+// Shared memory of a selecting CTA.
+template <int kThreads>
+struct SelectShared {
+    static constexpr int kFewMost = kThreads;        // tokens that are ranked against each other
+    uint32_t hist[kBins][32];                        // later: the keys that are ranked
+    uint32_t count[kBins];
+    uint32_t found[3];                               // the digit of the last one that stays, tokens above it, tokens with it
+    uint32_t few;
+    uint32_t warp_above[32], warp_equal[32];
+};
 
-// kEach: masses a thread keeps in registers (0: they are read again from memory for every pass)
-// Short contexts (kEach = 4) leave room for two CTAs on an SM: 32 x 32 heads of 500 ... 1000 tokens 39.5 -> 32.1 us, 64 x 32 76 -> 61 us, move
-// included.  (Longer ones with the upper halves of their keys in shared memory and two CTAs, so that registers suffice: 388 against 347 us for
-// the call above.  One kernel that selects and moves, two CTAs on an SM: 408 us.)
-template <int kEach>
-__global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_select_kernel(EvictArgs a)
+// Of the tokens c_lo ... c_hi - 1, the `need` that stay (fewer than there are), to `kept`.
+template <int kThreads, int kEach>
+__device__ __forceinline__ void select_tokens(const float* mass, int c_lo, int c_hi, uint32_t need, int32_t* kept, SelectShared<kThreads>& sm)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ uint32_t hist[kBins][32];             // later: the keys that are ranked
-    __shared__ uint32_t count[kBins];
-    __shared__ uint32_t found[3];                    // the digit of the last one that stays, tokens above it, tokens with it
-    __shared__ uint32_t few;
-    __shared__ uint32_t warp_above[kSelectWarps], warp_equal[kSelectWarps];
+    constexpr int kWarps = kThreads / 32;
+    auto& hist = sm.hist;
+    auto& count = sm.count;
+    auto& found = sm.found;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int s = blockIdx.x / a.sh.n_kv_heads;
-    const int64_t n64 = a.seq_lens[s];
-    const int n = (int)(n64 < 0 ? 0 : (n64 > a.sh.max_tokens ? a.sh.max_tokens : n64));
-    const float* mass = a.mass + (int64_t)blockIdx.x * a.sh.max_tokens;
-    int32_t* kept = a.kept + (int64_t)blockIdx.x * a.n_keep;
-    if (n <= a.n_keep) {
-        for (int j = threadIdx.x; j < a.n_keep; j += kSelectThreads) kept[j] = j < n ? j : -1;
-        return;
-    }
-    const int c_lo = a.n_sinks, c_hi = n - a.n_recent;                        // the tokens that compete
-    for (int j = threadIdx.x; j < a.n_sinks; j += kSelectThreads) kept[j] = j;
-    for (int j = threadIdx.x; j < a.n_recent; j += kSelectThreads) kept[a.n_keep - a.n_recent + j] = c_hi + j;
-    kept += a.n_sinks;
-    uint32_t need = (uint32_t)(a.n_keep - a.n_sinks - a.n_recent);            // how many of them stay (fewer than there are)
-    if (need == 0u) return;
     // warp w goes through the tokens from c_lo + w * turns * 32 on, turn j of lane l takes token j * 32 + l of them
-    const int turns = (c_hi - c_lo + kSelectThreads - 1) / kSelectThreads;
+    const int turns = (c_hi - c_lo + kThreads - 1) / kThreads;
     const int base = c_lo + warp * turns * 32 + lane;
     auto load = [&](int j) {                                                  // 0: no token (no mass has that key)
         const int t = base + 32 * j;
@@ -91,13 +78,13 @@ __global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_sele
     bool all = false;
     uint32_t least = 0u, mask = 0u;
     auto digit = [&](int shift) {                                             // finds the next eight bits
-        for (int i = threadIdx.x; i < kBins * 32; i += kSelectThreads) (&hist[0][0])[i] = 0u;
+        for (int i = threadIdx.x; i < kBins * 32; i += kThreads) (&hist[0][0])[i] = 0u;
         __syncthreads();
         each([&](int, uint32_t k) {
             if (k != 0u && (k & mask) == least) atomicAdd(&hist[(k >> shift) & (kBins - 1)][lane], 1u);
         });
         __syncthreads();
-        for (int bin = warp; bin < kBins; bin += kSelectWarps) {
+        for (int bin = warp; bin < kBins; bin += kWarps) {
             const uint32_t sum = __reduce_add_sync(0xffffffffu, hist[bin][lane]);
             if (lane == 0) count[bin] = sum;
         }
@@ -132,18 +119,18 @@ __global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_sele
     };
     digit(24);
     if (!all) digit(16);
-    if (!all && found[2] > kFewMost) digit(8);
-    if (!all && found[2] > kFewMost) digit(0);
+    if (!all && found[2] > SelectShared<kThreads>::kFewMost) digit(8);
+    if (!all && found[2] > SelectShared<kThreads>::kFewMost) digit(0);
     if (!all && mask != 0xffffffffu) {
         // few share the digits: each is ranked against the others
         uint32_t* keys = &hist[0][0];
-        if (threadIdx.x == 0) few = 0u;
+        if (threadIdx.x == 0) sm.few = 0u;
         __syncthreads();
         each([&](int, uint32_t k) {
-            if ((k & mask) == least) keys[atomicAdd(&few, 1u)] = k;           // (not 0: `least` has its highest digits)
+            if ((k & mask) == least) keys[atomicAdd(&sm.few, 1u)] = k;           // (not 0: `least` has its highest digits)
         });
         __syncthreads();
-        const uint32_t total = few;
+        const uint32_t total = sm.few;
         if (threadIdx.x < total) {
             const uint32_t k = keys[threadIdx.x];
             uint32_t above = 0u, equal = 0u;
@@ -171,10 +158,10 @@ __global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_sele
     });
     n_above = __reduce_add_sync(0xffffffffu, n_above);
     n_equal = __reduce_add_sync(0xffffffffu, n_equal);
-    if (lane == 0) { warp_above[warp] = n_above; warp_equal[warp] = n_equal; }
+    if (lane == 0) { sm.warp_above[warp] = n_above; sm.warp_equal[warp] = n_equal; }
     __syncthreads();
-    uint32_t above_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_above[lane] : 0u);
-    uint32_t equal_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_equal[lane] : 0u);
+    uint32_t above_before = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_above[lane] : 0u);
+    uint32_t equal_before = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_equal[lane] : 0u);
     const uint32_t below = (1u << lane) - 1u;
     if (all) {
         each([&](int j, uint32_t k) {
@@ -193,6 +180,40 @@ __global__ void __launch_bounds__(kSelectThreads, kEach == 4 ? 2 : 1) evict_sele
             equal_before += __popc(eq);
         });
     }
+}
+
+// kEach: masses a thread keeps in registers (0: they are read again from memory for every pass), kCtas: CTAs of an SM.  The unrolled loops are
+// those of the smallest of three numbers of turns that the sequence needs: 32 x 40 heads of 8192 ... 32768 tokens, move included, 347 us
+// with 32 turns for all, 307 with 16, 24 and 32, 309 with two or four more (the code grows); 8 heads of 4097 tokens 13.9 and 11.1 us.
+// (Upper halves of the keys in shared memory and two CTAs on an SM: 388 us.  One kernel that selects and moves: 408 us.)
+template <int kThreads, int kEach, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas) evict_select_kernel(EvictArgs a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ SelectShared<kThreads> sm;
+    const int s = blockIdx.x / a.sh.n_kv_heads;
+    const int64_t n64 = a.seq_lens[s];
+    const int n = (int)(n64 < 0 ? 0 : (n64 > a.sh.max_tokens ? a.sh.max_tokens : n64));
+    const float* mass = a.mass + (int64_t)blockIdx.x * a.sh.max_tokens;
+    int32_t* kept = a.kept + (int64_t)blockIdx.x * a.n_keep;
+    if (n <= a.n_keep) {
+        for (int j = threadIdx.x; j < a.n_keep; j += kThreads) kept[j] = j < n ? j : -1;
+        return;
+    }
+    const int c_lo = a.n_sinks, c_hi = n - a.n_recent;                        // the tokens that compete
+    for (int j = threadIdx.x; j < a.n_sinks; j += kThreads) kept[j] = j;
+    for (int j = threadIdx.x; j < a.n_recent; j += kThreads) kept[a.n_keep - a.n_recent + j] = c_hi + j;
+    kept += a.n_sinks;
+    const uint32_t need = (uint32_t)(a.n_keep - a.n_sinks - a.n_recent);
+    if (need == 0u) return;
+    const int turns = (c_hi - c_lo + kThreads - 1) / kThreads;
+    if constexpr (kEach > 4) {
+        constexpr int kLow = kEach == 32 ? 16 : kEach / 4, kMid = kEach == 32 ? 24 : kEach / 2;
+        if (turns <= kLow) return select_tokens<kThreads, kLow>(mass, c_lo, c_hi, need, kept, sm);
+        if (turns <= kMid) return select_tokens<kThreads, kMid>(mass, c_lo, c_hi, need, kept, sm);
+    }
+    select_tokens<kThreads, kEach>(mass, c_lo, c_hi, need, kept, sm);
 }
 
 constexpr int kMoveWarps = 8;
@@ -281,13 +302,17 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
 {
     const int64_t items = a.sh.n_seq * a.sh.n_kv_heads;
-    cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = overlapped_config((unsigned)items, kSelectThreads, 0, st, &attr);
-    cudaError_t e;
-    if (a.sh.max_tokens <= 4 * kSelectThreads) e = cudaLaunchKernelEx(&cfg, evict_select_kernel<4>, a);
-    else if (a.sh.max_tokens <= 16 * kSelectThreads) e = cudaLaunchKernelEx(&cfg, evict_select_kernel<16>, a);
-    else if (a.sh.max_tokens <= 32 * kSelectThreads) e = cudaLaunchKernelEx(&cfg, evict_select_kernel<32>, a);
-    else e = cudaLaunchKernelEx(&cfg, evict_select_kernel<0>, a);
+    auto select = [&](auto kernel, int threads) {
+        cudaLaunchAttribute attr;
+        const cudaLaunchConfig_t cfg = overlapped_config((unsigned)items, threads, 0, st, &attr);
+        return cudaLaunchKernelEx(&cfg, kernel, a);
+    };
+    // By capacity; where short ones are many, smaller CTAs, four on an SM: 32 x 32 heads of 500 ... 1000 tokens 24.6 us (one CTA 39.5, two of
+    // 1024 threads 32.1), 64 x 32 heads 45.8 (76, 61), move included.
+    const int64_t cap = a.sh.max_tokens;
+    const cudaError_t e = cap <= 4096 ? (items >= 2 * device_sm_count() ? select(evict_select_kernel<512, 8, 4>, 512) : select(evict_select_kernel<1024, 4, 1>, 1024))
+                          : cap <= 16384 ? select(evict_select_kernel<1024, 16, 1>, 1024)
+                          : cap <= 32768 ? select(evict_select_kernel<1024, 32, 1>, 1024) : select(evict_select_kernel<1024, 0, 1>, 1024);
     if (e != cudaSuccess) return e;
     const bool in_place = a.k_out == a.kc;
     const int64_t most = a.n_keep < a.sh.max_tokens ? a.n_keep : a.sh.max_tokens;

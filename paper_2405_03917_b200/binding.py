@@ -708,22 +708,19 @@ def cq_evict(mass: torch.Tensor, k_codes: torch.Tensor, v_codes: torch.Tensor, s
     """Keeps, per (sequence, head), the n_sinks first tokens, the n_recent last and the heaviest of the others, n_keep in all; mass fp32
     (n_seq, n_heads, max_tokens).  In place, or into a cache of capacity out_max_tokens (all three outputs given).  Returns
     (kept int32 (n_seq, n_heads, n_keep): old positions, -1 behind the last; the new lengths int32 (n_seq,))."""
-    n_seq, n_heads, _ = mass.shape
-    given = [t is not None for t in (k_codes_out, v_codes_out, mass_out)]
-    if any(given) and not all(given):
-        raise ValueError("k_codes_out, v_codes_out and mass_out come together")
-    if not any(given):
+    if k_codes_out is None and v_codes_out is None and mass_out is None:
         k_codes_out, v_codes_out, mass_out = k_codes, v_codes, mass
+    elif k_codes_out is None or v_codes_out is None or mass_out is None:
+        raise ValueError("k_codes_out, v_codes_out and mass_out come together")
     room = max_tokens if out_max_tokens is None else out_max_tokens
-    if mass.is_cuda:
-        kept = torch.empty(n_seq, n_heads, n_keep, dtype=torch.int32, device=mass.device) if kept is None and n_keep > 0 else kept
-        seq_lens_out = torch.empty(n_seq, dtype=torch.int32, device=mass.device) if seq_lens_out is None else seq_lens_out
-    st = (_native_module or _native()).evict(mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, room, mass_out,
-                                             k_codes_out, v_codes_out, kept, seq_lens_out)
-    if st is not None:
+    done = (_native_module or _native()).evict(mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, room, mass_out,
+                                               k_codes_out, v_codes_out, kept, seq_lens_out)
+    if done is not None:
+        st, kept, seq_lens_out = done
         if st:
             raise CQError(st, "cq_evict")
         return kept, seq_lens_out
+    n_seq, n_heads, _ = mass.shape
     _hold(cq_codes_bytes(n_seq, max_tokens, n_heads, head_dim, c, b), k_codes=k_codes, v_codes=v_codes)
     _hold(cq_codes_bytes(n_seq, room, n_heads, head_dim, c, b), k_codes_out=k_codes_out, v_codes_out=v_codes_out)
     with _one_device(mass, k_codes, v_codes, seq_lens, k_codes_out, v_codes_out, mass_out, kept, seq_lens_out):

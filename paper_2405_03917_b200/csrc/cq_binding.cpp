@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -307,7 +308,23 @@ PyObject* attn_mass(PyObject*, PyObject* const* argv, Py_ssize_t n)
                 ws->data_ptr(), (size_t)ws->numel(), variant, current_stream());
 }
 
-// mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, out_max_tokens, mass_out, k_out, v_out, kept, lens_out
+// An int32 tensor of the call's results: the given one, or a new one beside `like` where the argument is None.  (A new reference; made ahead of
+// the call, so that nothing throws behind it.)
+struct Result {
+    PyObject* object = nullptr;
+    const at::Tensor* tensor = nullptr;
+    Result(Args& a, int i, at::IntArrayRef shape, const at::Tensor& like)
+    {
+        if (a.a[i] == Py_None) object = THPVariable_Wrap(at::empty(shape, like.options().dtype(kInt)));
+        else if (a.device(i, kInt)) object = Py_NewRef(a.a[i]);
+        else return;
+        if (object) tensor = &THPVariable_Unpack(object);
+    }
+    ~Result() { Py_XDECREF(object); }
+};
+
+// mass, k_codes, v_codes, seq_lens, head_dim, c, b, max_tokens, n_keep, n_sinks, n_recent, out_max_tokens, mass_out, k_out, v_out, kept | None,
+// lens_out | None; returns (status, kept, lens_out)
 PyObject* evict(PyObject*, PyObject* const* argv, Py_ssize_t n)
 {
     if (n != 17) Py_RETURN_NONE;
@@ -315,15 +332,22 @@ PyObject* evict(PyObject*, PyObject* const* argv, Py_ssize_t n)
     const at::Tensor *m = a.device(0, kFloat), *kc = a.device(1, kByte), *vc = a.device(2, kByte), *sl = a.device(3, kInt);
     const int D = a.small(4), c = a.small(5), b = a.small(6);
     const int64_t cap = a.integer(7), keep = a.integer(8), sinks = a.integer(9), recent = a.integer(10), room = a.integer(11);
-    const at::Tensor *mo = a.device(12, kFloat), *ko = a.device(13, kByte), *vo = a.device(14, kByte), *kept = a.device(15, kInt), *lo = a.device(16, kInt);
-    if (!a.ok || m->dim() != 3 || !on_current_device({m, kc, vc, sl, mo, ko, vo, kept, lo})) Py_RETURN_NONE;
+    const at::Tensor *mo = a.device(12, kFloat), *ko = a.device(13, kByte), *vo = a.device(14, kByte);
+    if (!a.ok || m->dim() != 3 || keep <= 0 || !on_current_device({m, kc, vc, sl, mo, ko, vo})) Py_RETURN_NONE;
     const int64_t ns = m->size(0), h = m->size(1);
-    if (!is_shape(*m, {ns, h, cap}) || !is_shape(*mo, {ns, h, room}) || sl->numel() != ns || !is_shape(*kept, {ns, h, keep}) || !is_shape(*lo, {ns}) ||
-        !hold_codes(*kc, *vc, ns, cap, h, D, c, b) || !hold_codes(*ko, *vo, ns, room, h, D, c, b))
+    if (!is_shape(*m, {ns, h, cap}) || !is_shape(*mo, {ns, h, room}) || sl->numel() != ns || !hold_codes(*kc, *vc, ns, cap, h, D, c, b) ||
+        !hold_codes(*ko, *vo, ns, room, h, D, c, b))
         Py_RETURN_NONE;
-    return call(cq_evict, (const float*)m->data_ptr(), kc->data_ptr(), vc->data_ptr(), (const int32_t*)sl->data_ptr(), (int)ns, (int)h, D, c, b, cap, keep,
-                sinks, recent, room, (float*)mo->data_ptr(), ko->data_ptr(), vo->data_ptr(), (int32_t*)kept->data_ptr(), (int32_t*)lo->data_ptr(),
-                current_stream());
+    const Result kept(a, 15, {ns, h, keep}, *m), left(a, 16, {ns}, *m);
+    if (!kept.tensor || !left.tensor) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (!is_shape(*kept.tensor, {ns, h, keep}) || !is_shape(*left.tensor, {ns}) || !on_current_device({kept.tensor, left.tensor})) Py_RETURN_NONE;
+    int32_t *to_kept = (int32_t*)kept.tensor->data_ptr(), *to_left = (int32_t*)left.tensor->data_ptr();
+    PyObject* status = call(cq_evict, (const float*)m->data_ptr(), kc->data_ptr(), vc->data_ptr(), (const int32_t*)sl->data_ptr(), (int)ns, (int)h, D, c, b,
+                            cap, keep, sinks, recent, room, (float*)mo->data_ptr(), ko->data_ptr(), vo->data_ptr(), to_kept, to_left, current_stream());
+    return Py_BuildValue("(NOO)", status, kept.object, left.object);
 }
 
 // torch throws where a tensor has no memory (under tracing or vmap) or no current stream: no exception may leave for the

@@ -9,7 +9,7 @@
 //       Masses crowd in few bins: every lane counts in a column of its own, so that the lanes of a warp never meet.  What bounds it is
 //       the number of instructions per token: 32 sequences x 40 heads of 8192 ... 32768 tokens: 345 us with a shared column per bin
 //       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, 161 us with masses in
-//       registers, room for the longest, 120 us with a loop for each of three lengths (105 MB of masses: 16 us).
+//       registers, room for the longest, 116 us with a loop for each of three lengths (105 MB of masses: 16 us).
 //   evict_move_kernel    a warp per 16 tokens that stay: a lane takes one (tensor, group) of them, a byte load per token (the
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
 //       187 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
@@ -117,10 +117,12 @@ __device__ __forceinline__ void select_tokens(const float* mass, int c_lo, int c
         all = need == found[2];                                               // the digits so far tell those that stay from the others
         __syncthreads();
     };
-    digit(24);
-    if (!all) digit(16);
-    if (!all && found[2] > SelectShared<kThreads>::kFewMost) digit(8);
-    if (!all && found[2] > SelectShared<kThreads>::kFewMost) digit(0);
+    // (one copy of the unrolled loop for all digits: the instructions of four came late, 307 against 303 us and 24.6 against 22.0)
+#pragma unroll 1
+    for (int shift = 24;; shift -= 8) {
+        digit(shift);
+        if (all || shift == 0 || (shift <= 16 && found[2] <= SelectShared<kThreads>::kFewMost)) break;
+    }
     if (!all && mask != 0xffffffffu) {
         // few share the digits: each is ranked against the others
         uint32_t* keys = &hist[0][0];
@@ -184,7 +186,7 @@ __device__ __forceinline__ void select_tokens(const float* mass, int c_lo, int c
 
 // kEach: masses a thread keeps in registers (0: they are read again from memory for every pass), kCtas: CTAs of an SM.  The unrolled loops are
 // those of the smallest of three numbers of turns that the sequence needs: 32 x 40 heads of 8192 ... 32768 tokens, move included, 347 us
-// with 32 turns for all, 307 with 16, 24 and 32, 309 with two or four more (the code grows); 8 heads of 4097 tokens 13.9 and 11.1 us.
+// with 32 turns for all, 303 with 16, 24 and 32 (two or four more: slower by 1 %, the code grows); 8 heads of 4097 tokens 13.9 and 10.8 us.
 // (Upper halves of the keys in shared memory and two CTAs on an SM: 388 us.  One kernel that selects and moves: 408 us.)
 template <int kThreads, int kEach, int kCtas>
 __global__ void __launch_bounds__(kThreads, kCtas) evict_select_kernel(EvictArgs a)
@@ -307,8 +309,8 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
         const cudaLaunchConfig_t cfg = overlapped_config((unsigned)items, threads, 0, st, &attr);
         return cudaLaunchKernelEx(&cfg, kernel, a);
     };
-    // By capacity; where short ones are many, smaller CTAs, four on an SM: 32 x 32 heads of 500 ... 1000 tokens 24.6 us (one CTA 39.5, two of
-    // 1024 threads 32.1), 64 x 32 heads 45.8 (76, 61), move included.
+    // By capacity; where short ones are many, smaller CTAs, four on an SM: 32 x 32 heads of 500 ... 1000 tokens 22.0 us (one CTA 39.5, two of
+    // 1024 threads 32.1), 64 x 32 heads 40.2 (76, 61), move included.
     const int64_t cap = a.sh.max_tokens;
     const cudaError_t e = cap <= 4096 ? (items >= 2 * device_sm_count() ? select(evict_select_kernel<512, 8, 4>, 512) : select(evict_select_kernel<1024, 4, 1>, 1024))
                           : cap <= 16384 ? select(evict_select_kernel<1024, 16, 1>, 1024)

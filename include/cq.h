@@ -440,7 +440,9 @@ int cq_decode_step_host(const void *q_host, const void *k_new_host, const void *
  * seq_lens counts them): query i of n sits at position seq_lens[s] - n + i.  A query at position p sees cached token t where
  *     t <= p   and   (window == 0  or  t < n_sinks  or  t > p - window),
  * so window counts the query's own token, and the n_sinks first tokens stay visible behind the window.  A query that sees
- * nothing (its position is negative, or no page is named for what it sees) gets a zero row.
+ * nothing (its position is negative, or no page is named for what it sees) gets a zero row.  A query with a NaN gets a row of
+ * NaN, and so do the masses that it adds to; other rows are not touched by it.  Centroids have to be finite: a weight of zero
+ * does not hide an infinite value.
  *
  * Kernels.  head_dim 128 with one byte per code, c = 2, 4 or 8: sequences with up to 16 (query token, query head of a KV head)
  * rows go through a kernel whose warps gather centroids from shared memory straight into tensor-core fragments, sequences
@@ -520,7 +522,8 @@ int cq_paged_append(const void *k_fp16, const void *v_fp16, const int32_t *q_off
  *   mass_out     the same shape, may be mass_in; positions from seq_lens[s] on are left as they were
  *   workspace    cq_attn_mass_workspace_bytes(...) bytes, 16-byte aligned.  For up to four rows (query tokens x query heads of a
  *                KV head) they hold the scores between the two passes, 16 bytes per cached token and KV head.  What the same call
- *                with max_tokens = n_q_tokens asks for is enough: the second pass then works the scores out again
+ *                with max_tokens = n_q_tokens asks for is enough for these: the second pass then works the scores out again.
+ *                (Above 256 rows they hold the sums of every 256, 4 bytes per cached token and KV head.)
  * Sums are formed in a fixed order: two calls on the same inputs give the same bits.
  * variant: as above (up to 16 rows of a sequence and KV head take the gather kernel, more the tcgen05 one).
  */

@@ -1,5 +1,5 @@
 // Attention of many query rows over a bounded cache (window, sinks, pages, ragged rows), and the masses that they give to cached tokens:
-// the bounded forms of the tensor-core kernel in cq_prefill_tc.cuh, and what joins the parts of a context or the row tiles.
+// the bounded forms of the tensor-core kernel in cq_prefill_tc.cu, and what joins the parts of a context or the row tiles.
 //
 // Attention.  What bounds it: per 64 tokens and 256 rows the MMAs take 1024 cycles of about 2160.  The rest is a chain: scores of a row tile
 // (tensor memory has room for one tile of them beside the outputs, queries and weights), their way into registers, the other row tile's
@@ -13,7 +13,7 @@
 // warps through shared memory, over row tiles in a kernel of its own; every sum has one order.  What bounds it: the exponentials (two
 // passes, 16 per clock and SM) and the waits behind them: 1190 and 1660 cycles per 64 tokens of 128 rows.  A second tile of scores in the
 // outputs' columns changed nothing.  4 x 32 queries over 5001 ... 8192 tokens, 32 heads on 8, CQ-8c8b: 63 us, 227 us with the gather kernel.
-#include "cq_prefill_tc.cuh"
+#include "cq_prefill_tc.cu"
 
 namespace cq {
 

@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32) evict_move_kernel(EvictArgs a
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
 {
     const int64_t items = a.sh.n_seq * a.sh.n_kv_heads;
-    auto select = [&](auto kernel, int threads) {
+    auto go = [&](auto kernel, int threads) {
         cudaLaunchAttribute attr;
         const cudaLaunchConfig_t cfg = overlapped_config((unsigned)items, threads, 0, st, &attr);
         return cudaLaunchKernelEx(&cfg, kernel, a);
@@ -312,20 +312,20 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t st)
     // By capacity; where short ones are many, smaller CTAs, four on an SM: 32 x 32 heads of 500 ... 1000 tokens 22.0 us (one CTA 39.5, two of
     // 1024 threads 32.1), 64 x 32 heads 40.2 (76, 61), move included.
     const int64_t cap = a.sh.max_tokens;
-    const cudaError_t e = cap <= 4096 ? (items >= 2 * device_sm_count() ? select(evict_select_kernel<512, 8, 4>, 512) : select(evict_select_kernel<1024, 4, 1>, 1024))
-                          : cap <= 16384 ? select(evict_select_kernel<1024, 16, 1>, 1024)
-                          : cap <= 32768 ? select(evict_select_kernel<1024, 32, 1>, 1024) : select(evict_select_kernel<1024, 0, 1>, 1024);
+    const cudaError_t e = cap <= 4096 ? (items >= 2 * device_sm_count() ? go(evict_select_kernel<512, 8, 4>, 512) : go(evict_select_kernel<1024, 4, 1>, 1024))
+                          : cap <= 16384 ? go(evict_select_kernel<1024, 16, 1>, 1024)
+                          : cap <= 32768 ? go(evict_select_kernel<1024, 32, 1>, 1024) : go(evict_select_kernel<1024, 0, 1>, 1024);
     if (e != cudaSuccess) return e;
     const bool in_place = a.k_out == a.kc;
     const int64_t most = a.n_keep < a.sh.max_tokens ? a.n_keep : a.sh.max_tokens;
     const int n_out = (int)((most + kTokenBlock - 1) / kTokenBlock);
     int per_cta = in_place ? n_out : 4 * kMoveWarps;
     while ((n_out + per_cta - 1) / per_cta > 65535) per_cta *= 2;
-    cudaLaunchAttribute attr2;
-    cudaLaunchConfig_t move = overlapped_config((unsigned)items, kMoveWarps * 32, 0, st, &attr2);
-    move.gridDim = dim3((unsigned)items, (unsigned)((n_out + per_cta - 1) / per_cta));
-    if (a.sh.hb) return in_place ? cudaLaunchKernelEx(&move, evict_move_kernel<true, true>, a, per_cta) : cudaLaunchKernelEx(&move, evict_move_kernel<true, false>, a, per_cta);
-    return in_place ? cudaLaunchKernelEx(&move, evict_move_kernel<false, true>, a, per_cta) : cudaLaunchKernelEx(&move, evict_move_kernel<false, false>, a, per_cta);
+    cudaLaunchAttribute attr;
+    cudaLaunchConfig_t cfg = overlapped_config((unsigned)items, kMoveWarps * 32, 0, st, &attr);
+    cfg.gridDim = dim3((unsigned)items, (unsigned)((n_out + per_cta - 1) / per_cta));
+    if (a.sh.hb) return in_place ? cudaLaunchKernelEx(&cfg, evict_move_kernel<true, true>, a, per_cta) : cudaLaunchKernelEx(&cfg, evict_move_kernel<true, false>, a, per_cta);
+    return in_place ? cudaLaunchKernelEx(&cfg, evict_move_kernel<false, true>, a, per_cta) : cudaLaunchKernelEx(&cfg, evict_move_kernel<false, false>, a, per_cta);
 }
 
 }  // namespace cq

@@ -8,7 +8,7 @@
 // With many queries per cached token the per-query lookup tables of the decode kernels no longer
 // pay (one table per query); the codes are turned back into vectors instead and the two
 // contractions run on the tensor cores:
-//   prefill_tc_kernel (cq_prefill_tc.cuh; head_dim 128, one byte per code, c = 2, 4 or 8): one CTA per (sequence, KV
+//   prefill_tc_kernel (cq_prefill_tc.cu; head_dim 128, one byte per code, c = 2, 4 or 8): one CTA per (sequence, KV
 //     head, 256 (query, head of the KV head's group) rows), as two row tiles of 128, one row per lane
 //     of tensor memory.  Both codebooks are kept in shared memory as fp16, code-major, so that the
 //     lanes of a gather (one group each) meet in no bank whatever the codes are.  Four producer warps
@@ -21,7 +21,7 @@
 //     tiles' fragments in registers, 1.36 ms with one MMA-issuing thread that did scores and sums in
 //     turn, 0.95 ms now, 0.57 ms being the contractions at the measured GEMM rate.
 //   prefill_generic_kernel: any supported shape, one CTA per (sequence, query, head), plain loops.
-#include "cq_prefill_tc.cuh"
+#include "cq_prefill_tc.cu"
 
 namespace cq {
 

@@ -1,5 +1,6 @@
 // Tensor-core kernel of the attention of many query rows over a coded cache (head_dim 128, one byte per code): device code shared
-// by the causal attention over a contiguous cache (cq_prefill.cu) and by the operators on bounded caches (cq_chunk_attn.cu).
+// by the causal attention over a contiguous cache (cq_prefill.cu) and by the operators on bounded caches (cq_chunk_attn.cu), which include
+// this file; it is not compiled by itself.
 #pragma once
 
 #include <type_traits>

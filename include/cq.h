@@ -486,6 +486,9 @@ int cq_window_attn_variant(const void *q_fp16, const void *k_codes, const void *
  *                entry outside of [0, n_pages) count as absent
  *   seq_lens     [n_seq] int32, device: cached tokens, the new ones included
  *   window, n_sinks   as above; window 0: all tokens
+ *   workspace    at least cq_paged_attn_workspace_bytes(...) bytes for the arguments of the call, 16-byte aligned.  (A batch of
+ *                fewer rows can ask for more: its contexts are shared by more CTAs.  No batch asks for more than 133120 bytes for
+ *                each of the GPU's SMs.)
  */
 size_t cq_paged_attn_workspace_bytes(int n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_kv_heads, int head_dim, int c,
                                      int b, int64_t page_tokens, int64_t pages_per_seq, int64_t window, int64_t n_sinks);

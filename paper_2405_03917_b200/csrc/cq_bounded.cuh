@@ -108,8 +108,8 @@ cudaError_t launch_gather_mass(const BoundedArgs& a, const float* mass_in, float
 
 // many rows per sequence (cq_chunk_attn.cu): the tensor-core kernel of the prefill attention in its bounded form
 bool chunk_attn_supported(const Shape& sh);
-size_t chunk_attn_workspace_bytes(const BoundedArgs& a);
-cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, cudaStream_t st);
+size_t chunk_attn_workspace_bytes(const BoundedArgs& a);        // (goes by least_rows as well: ask for the arguments of the launch)
+cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, size_t workspace_bytes, cudaStream_t st);
 // the masses that they give (uniform rows, a contiguous cache, no window)
 size_t chunk_mass_workspace_bytes(const BoundedArgs& a);
 cudaError_t launch_chunk_mass(const BoundedArgs& a, const float* mass_in, float* mass_out, void* workspace, cudaStream_t st);

@@ -52,14 +52,22 @@ int paged_shape(int64_t n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_k
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 int status(cudaError_t e) { return e == cudaSuccess ? CQ_OK : CQ_ERR_CUDA; }
 
-int run_attn(BoundedArgs a, int variant, void* workspace, cudaStream_t st)
+// What of a ragged batch is the tensor-core kernel's beside the gather kernel: the sequences with more rows than that takes.  Its plan goes by
+// this (fewer row tiles leave more CTAs for each), so the workspace is asked for, checked and laid out for the same arguments.
+BoundedArgs many_rows(BoundedArgs a)
+{
+    a.least_rows = kFewRows + 1;
+    return a;
+}
+
+int run_attn(BoundedArgs a, int variant, void* workspace, size_t workspace_bytes, cudaStream_t st)
 {
     if (variant < 0 || variant > 3) return CQ_ERR_SHAPE;
     const bool gather = gather_attn_supported(a.sh), chunk = chunk_attn_supported(a.sh);
     if ((variant == 2 && !gather) || (variant == 3 && !chunk)) return CQ_ERR_UNSUPPORTED;
     if (a.n_rows == 0) return CQ_OK;
     if (variant == 2) return status(launch_gather_attn(a, workspace, st));
-    if (variant == 3) return status(launch_chunk_attn(a, workspace, st));
+    if (variant == 3) return status(launch_chunk_attn(a, workspace, workspace_bytes, st));
     if (variant == 1 || !gather || !chunk) return status(launch_bounded_plain(a, st));
     // every sequence takes the kernel of its number of rows; without ragged rows that is the same one for all
     if ((int64_t)a.max_q * a.sh.R <= kFewRows) return status(launch_gather_attn(a, workspace, st));
@@ -68,15 +76,19 @@ int run_attn(BoundedArgs a, int variant, void* workspace, cudaStream_t st)
         few.most_rows = kFewRows;
         const cudaError_t e = launch_gather_attn(few, workspace, st);
         if (e != cudaSuccess) return CQ_ERR_CUDA;
-        a.least_rows = kFewRows + 1;
+        a = many_rows(a);
     }
-    return status(launch_chunk_attn(a, workspace, st));
+    return status(launch_chunk_attn(a, workspace, workspace_bytes, st));
 }
-size_t attn_workspace(const BoundedArgs& a)
+size_t attn_workspace(const BoundedArgs& a, bool ragged)
 {
-    size_t bytes = 256;
-    if (gather_attn_supported(a.sh) && gather_attn_workspace_bytes() > bytes) bytes = gather_attn_workspace_bytes();
-    if (chunk_attn_supported(a.sh) && chunk_attn_workspace_bytes(a) > bytes) bytes = chunk_attn_workspace_bytes(a);
+    size_t bytes = 256;                                                        // enough for every kernel that the shape has
+    auto room_for = [&](size_t need) { bytes = need > bytes ? need : bytes; };
+    if (gather_attn_supported(a.sh)) room_for(gather_attn_workspace_bytes());
+    if (chunk_attn_supported(a.sh)) {
+        room_for(chunk_attn_workspace_bytes(a));
+        if (ragged) room_for(chunk_attn_workspace_bytes(many_rows(a)));
+    }
     return bytes;
 }
 
@@ -90,7 +102,7 @@ size_t cq_window_attn_workspace_bytes(int n_seq, int n_q_tokens, int n_q_heads, 
     BoundedArgs a;
     if (bounded_shape(n_seq, (int64_t)n_seq * n_q_tokens, n_q_tokens, max_tokens, n_q_heads, n_kv_heads, head_dim, c, b, window, n_sinks, &a) != CQ_OK)
         return 0;
-    return attn_workspace(a);
+    return attn_workspace(a, false);
 }
 
 int cq_window_attn_variant(const void* q_fp16, const void* k_codes, const void* v_codes, const void* k_cb_fp16, const void* v_cb_fp16,
@@ -105,7 +117,7 @@ int cq_window_attn_variant(const void* q_fp16, const void* k_codes, const void* 
     if (!aligned16(q_fp16) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_cb_fp16) || !aligned16(v_cb_fp16) ||
         !aligned16(out_fp16) || !aligned16(workspace) || !aligned4(seq_lens))
         return CQ_ERR_ALIGN;
-    if (workspace_bytes < attn_workspace(a)) return CQ_ERR_WORKSPACE;
+    if (workspace_bytes < attn_workspace(a, false)) return CQ_ERR_WORKSPACE;
     a.q = static_cast<const __half*>(q_fp16);
     a.kc = static_cast<const uint8_t*>(k_codes);
     a.vc = static_cast<const uint8_t*>(v_codes);
@@ -114,7 +126,7 @@ int cq_window_attn_variant(const void* q_fp16, const void* k_codes, const void* 
     a.seq_lens = seq_lens;
     a.scale_log2e = scale * kLog2e;
     a.out = static_cast<__half*>(out_fp16);
-    return run_attn(a, variant, workspace, static_cast<cudaStream_t>(stream));
+    return run_attn(a, variant, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 int cq_window_attn(const void* q_fp16, const void* k_codes, const void* v_codes, const void* k_cb_fp16, const void* v_cb_fp16,
@@ -131,7 +143,7 @@ size_t cq_paged_attn_workspace_bytes(int n_seq, int64_t n_rows, int max_q, int n
 {
     BoundedArgs a;
     if (paged_shape(n_seq, n_rows, max_q, n_q_heads, n_kv_heads, head_dim, c, b, 1, page_tokens, pages_per_seq, window, n_sinks, &a) != CQ_OK) return 0;
-    return attn_workspace(a);
+    return attn_workspace(a, true);
 }
 
 int cq_paged_attn_variant(const void* q_fp16, const int32_t* q_offsets, const void* k_pages, const void* v_pages, const void* k_cb_fp16,
@@ -148,7 +160,7 @@ int cq_paged_attn_variant(const void* q_fp16, const int32_t* q_offsets, const vo
     if (!aligned16(q_fp16) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_cb_fp16) || !aligned16(v_cb_fp16) ||
         !aligned16(out_fp16) || !aligned16(workspace) || !aligned4(seq_lens) || !aligned4(q_offsets) || !aligned4(page_table))
         return CQ_ERR_ALIGN;
-    if (workspace_bytes < attn_workspace(a)) return CQ_ERR_WORKSPACE;
+    if (workspace_bytes < attn_workspace(a, true)) return CQ_ERR_WORKSPACE;
     a.q = static_cast<const __half*>(q_fp16);
     a.kc = static_cast<const uint8_t*>(k_pages);
     a.vc = static_cast<const uint8_t*>(v_pages);
@@ -159,7 +171,7 @@ int cq_paged_attn_variant(const void* q_fp16, const int32_t* q_offsets, const vo
     a.page_table = page_table;
     a.scale_log2e = scale * kLog2e;
     a.out = static_cast<__half*>(out_fp16);
-    return run_attn(a, variant, workspace, static_cast<cudaStream_t>(stream));
+    return run_attn(a, variant, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 int cq_paged_attn(const void* q_fp16, const int32_t* q_offsets, const void* k_pages, const void* v_pages, const void* k_cb_fp16,

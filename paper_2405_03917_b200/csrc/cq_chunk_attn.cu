@@ -134,8 +134,9 @@ int row_tiles_of(const BoundedArgs& a) { const int q_per_tile = PfCfgB::kRows / 
 
 }  // namespace
 
-cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, cudaStream_t st)
+cudaError_t launch_chunk_attn(const BoundedArgs& a, void* workspace, size_t workspace_bytes, cudaStream_t st)
 {
+    if (workspace_bytes < chunk_attn_workspace_bytes(a)) return cudaErrorInvalidValue;       // (the caller has asked for another plan)
     const Plan p = plan_of(a);
     const int64_t items = p.tiles * a.sh.n_kv_heads;
     if (items * p.parts > 0x7fffffff || items * (PfCfgB::kRows / kMergeWarps) > 0x7fffffff) return cudaErrorInvalidConfiguration;

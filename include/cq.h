@@ -446,8 +446,9 @@ int cq_decode_step_host(const void *q_host, const void *k_new_host, const void *
  *
  * Kernels.  head_dim 128 with one byte per code, c = 2, 4 or 8: sequences with up to 16 (query token, query head of a KV head)
  * rows go through a kernel whose warps gather centroids from shared memory straight into tensor-core fragments, sequences
- * with more rows through one on tcgen05 (every wait in it is bounded; should one give up, its rows are NaN).  Softmax weights
- * are rounded to fp16 for the second product, sums are fp32.  Every other supported shape runs on plain kernels.
+ * with more rows through one on tcgen05 (every wait in it is bounded; should one give up, the rows or masses that it would have
+ * written are NaN).  Softmax weights are rounded to fp16 for the second product, sums are fp32.  Every other supported shape runs on
+ * plain kernels.
  * _variant picks: 0 = automatic, 1 = plain kernel, 2 = the gather kernel, 3 = the tcgen05 kernel (CQ_ERR_UNSUPPORTED where
  * the shape has none).
  */

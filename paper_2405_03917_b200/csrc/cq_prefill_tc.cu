@@ -110,6 +110,9 @@ __device__ __forceinline__ bool pf_wait(PfCtl* ctl, uint64_t* bar, uint32_t pari
     ctl->failed = 1;
     return false;
 }
+// Whether a wait of the CTA has given up.  Who has not waited arrives too early: from then on a barrier says nothing about the other threads' data
+// either.  (The word is written before such an arrival, so whoever reads on because of one finds it.)
+__device__ __forceinline__ bool pf_failed(const PfCtl* ctl) { return *reinterpret_cast<const volatile int*>(&ctl->failed) != 0; }
 
 // Shared-memory matrix descriptor of a tile of 128-byte rows with the 128-byte swizzle (16-byte chunk index XOR row mod 8).
 // Rows = tokens.  As keys (contraction along the row) eight rows are one core matrix group of 1024 bytes; as values (the
@@ -621,12 +624,13 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             const int64_t row_tile = bounded.row_tiles > 1 ? tile : 0;
             const int64_t base = ((row_tile * sh.n_seq + s) * sh.n_kv_heads + hkv) * sh.max_tokens;
             const bool old = bounded.mass_in && bounded.row_tiles == 1;
+            bool there = true;                                              // (a wait gave up: NaN for the tokens of this and all further tiles)
             for (int jt = 0; jt < n_tiles; ++jt) {
                 const int64_t t0 = (int64_t)tile_at(jt) * C::kTile + lane;
                 float sum[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) sum[k] = old && t0 + 32 * k < n ? bounded.mass_in[base + t0 + 32 * k] : 0.f;
-                if (!__all_sync(0xffffffffu, pf_wait(ctl, &ctl->p_full[lane % n_halves], (uint32_t)jt & 1u))) break;
+                if (there) there = __all_sync(0xffffffffu, pf_wait(ctl, &ctl->p_full[lane % n_halves], (uint32_t)jt & 1u) && !pf_failed(ctl));
                 float add[2] = {0.f, 0.f};
                 for (int i = 0; i < 4 * n_halves; ++i)
 #pragma unroll
@@ -635,7 +639,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 if (lane == 0) pf_arrive(&ctl->pv_done[0]);                 // the next ones may come
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
-                    if (t0 + 32 * k < n) bounded.mass_out[base + t0 + 32 * k] = sum[k] + add[k];
+                    if (t0 + 32 * k < n) bounded.mass_out[base + t0 + 32 * k] = there ? sum[k] + add[k] : __int_as_float(0x7fffffff);
             }
         }
     } else if (kSums && warp == C::kSumWarp) {
@@ -833,6 +837,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 }
             }
             if constexpr (kWhat == kPfLse) {                                // the two threads of a row to one
+                ok = !pf_pair_any(pair, !ok || pf_failed(ctl));
                 exchange[part * C::kRows + rho] = m;
                 pf_pair_sync(pair);
                 const float other = exchange[(part ^ 1) * C::kRows + rho], top = fmaxf(m, other);
@@ -853,7 +858,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 l += exchange[(part ^ 1) * C::kRows + rho];
                 // ---- normalise and write, through shared memory (the codebooks are done with when the last sums are), in whole lines
                 if (n_tiles > 0) ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(n_tiles - 1) & 1u);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = !pf_pair_any(pair, !ok || pf_failed(ctl));                 // (the rows' both halves)
                 pf_fence_after();
                 const bool partial = bounded.parts > 1;                         // (partials: the accumulators as they are)
                 // nothing seen: a zero row; a wait gave up: NaN rows, so that nothing takes them for a result

@@ -192,7 +192,7 @@ struct PfBounded {
     int tiles;                 // bound on the row tiles of all sequences
     int parts;                 // CTAs that share a row tile's context
     float* partials;           // attention, parts > 1: [CTA][256 rows][partial_stride(128)] (reference, sum, accumulators);
-                               // log-sum-exps: [CTA][256 rows][2]
+                               // log-sum-exps: [CTA][256 rows][2] (reference NaN: a wait gave up)
     const float* mass_in;      // masses: of one row tile per sequence, on top of these (may be null)
     float* mass_out;           // [sequence][KV head][max_tokens]; of several row tiles, [row tile][sequence][KV head][max_tokens]
     int row_tiles;
@@ -709,13 +709,19 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             bool ok = true;
             if constexpr (kWhat == kPfMass) {                               // the row's log-sum-exp, from the parts of its context
                 const float* of = bounded.partials + ((int64_t)(blockIdx.x / bounded.parts) * bounded.parts * C::kRows + rho) * 2;
-                for (int i = 0; i < bounded.parts; ++i) m = fmaxf(m, of[(int64_t)i * C::kRows * 2]);
+                bool gave_up = false;
+                for (int i = 0; i < bounded.parts; ++i) {
+                    const float mi = of[(int64_t)i * C::kRows * 2];
+                    gave_up |= mi != mi;
+                    m = fmaxf(m, mi);
+                }
                 for (int i = 0; i < bounded.parts; ++i) {
                     const float mi = of[(int64_t)i * C::kRows * 2];
                     l += (mi == -INFINITY ? 1.f : exp2f(mi - m)) * of[(int64_t)i * C::kRows * 2 + 1];      // (no reference: zero, or no number)
                 }
-                // (a row that sees nothing: no weight; a row that is none: none of its scores, which are zero, counts)
-                m = !(qi < n_q && rho < rows_used) ? INFINITY : l == 0.f ? 0.f : m + log2f(l);
+                // (a row that sees nothing: no weight; a row that is none: none of its scores, which are zero, counts; a sum that is no number comes from
+                // scores that are none, or infinite: they give NaN by themselves, and what the row does not see gets no weight)
+                m = !(qi < n_q && rho < rows_used) ? INFINITY : gave_up ? __int_as_float(0x7fffffff) : l == 0.f ? 0.f : l == l ? m + log2f(l) : m == -INFINITY ? 0.f : m;
             }
 #pragma unroll 1
             for (int jt = 0; jt < n_tiles; ++jt) {
@@ -846,8 +852,8 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
                 pf_pair_sync(pair);
                 if (part == 0) {
                     float* of = bounded.partials + ((int64_t)blockIdx.x * C::kRows + rho) * 2;
-                    of[0] = top;
-                    of[1] = ok ? l + exchange[C::kRows + rho] : __int_as_float(0x7fffffff);
+                    of[0] = ok ? top : __int_as_float(0x7fffffff);          // (a wait gave up: no reference is a number)
+                    of[1] = l + exchange[C::kRows + rho];
                 }
                 pf_fence_before();
             }

@@ -84,6 +84,14 @@ __device__ __forceinline__ bool token_visible(int t, int pos, int window, int si
 {
     return t <= pos && (window == 0 || t < sinks || t > pos - window);
 }
+// What queries are multiplied by ahead of the products, so that the scores' factor can be positive: the sign of the scale (1 and -1 are exact), zero
+// for a scale of zero (a query that is no number, or infinite, stays visible: NaN).
+__device__ __forceinline__ __half2 query_sign(float scale) { return __float2half2_rn(scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f); }
+__device__ __forceinline__ uint32_t signed_query(uint32_t two, __half2 sign)
+{
+    const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&two), sign);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
 // First token of the window of a query at pos (0 without a window).
 __device__ __forceinline__ int window_first(int pos, int window) { return window == 0 || pos < window ? 0 : pos - window + 1; }
 

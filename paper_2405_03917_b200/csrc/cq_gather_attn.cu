@@ -254,8 +254,7 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
     }
     // (before the next writer of scratch and of the cut records, the CTA has met again)
 
-    // a negative scale: the queries change sign instead; a zero one: they become zero; both are exact
-    const uint32_t q_sign = a.scale_log2e < 0.f ? 0x80008000u : 0u, q_keep = a.scale_log2e == 0.f ? 0u : 0xffffffffu;
+    const __half2 q_sign = query_sign(a.scale_log2e);
     const float scale = a.scale_log2e == 0.f ? 1.f : fabsf(a.scale_log2e);
 
     // ---- lane constants
@@ -487,7 +486,7 @@ gather_kernel(BoundedArgs a, MassArgs mass, float* __restrict__ partials, Cut* _
         uint32_t qf[4][kQF];
         {
             const uint32_t* qr = reinterpret_cast<const uint32_t*>(smem + C::kQOffset) + (kRows == 4 ? r >> 1 : r) * 64;
-            auto word = [&](int w, int h) { return (qr[(8 * (w / E) + 4 * h + p) * E + w % E] ^ q_sign) & q_keep; };       // w of half h
+            auto word = [&](int w, int h) { return signed_query(qr[(8 * (w / E) + 4 * h + p) * E + w % E], q_sign); };       // w of half h
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
                 if (kRows == 4) {

@@ -692,12 +692,13 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
             // a tile part that starts at j0 is seen whole by all rows of the warp up to seen_to, and from behind seen_from or up to seen_sinks
             const int seen_to = (int)pos0 + row0 / R - 31, seen_from = window ? (int)pos0 + (row0 + 31) / R - window : -1, seen_sinks = bounded.a.sinks - 32;
             {
+                const __half2 sign = query_sign(scale_log2e);
                 uint32_t u[32];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint4 v = *reinterpret_cast<const uint4*>(smem + C::q_offset(rho) + (((8 * part + i) ^ (rho & 7)) << 4));
-                    u[4 * i] = (v.x ^ q_sign) & q_keep; u[4 * i + 1] = (v.y ^ q_sign) & q_keep;
-                    u[4 * i + 2] = (v.z ^ q_sign) & q_keep; u[4 * i + 3] = (v.w ^ q_sign) & q_keep;
+                    u[4 * i] = signed_query(v.x, sign); u[4 * i + 1] = signed_query(v.y, sign);
+                    u[4 * i + 2] = signed_query(v.z, sign); u[4 * i + 3] = signed_query(v.w, sign);
                 }
                 pf_st32(lanes + C::kQCol + 64 * t + 32 * part, u);
                 pf_st_wait();

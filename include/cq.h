@@ -552,8 +552,8 @@ int cq_attn_mass_variant(const void *q_fp16, const void *k_codes, const void *k_
  *                block of codes is zeroed, everything behind it is left as it was.
  *   kept_out     int32 [n_seq][n_heads][n_keep]: the old position of every token that stays, ascending, -1 behind the last
  *   seq_lens_out [n_seq] int32, not seq_lens: min(n, n_keep)
- * Needs no workspace.  CQ_ERR_SHAPE for n_keep < 1 or > out_max_tokens, n_sinks + n_recent > n_keep, or buffers that alias
- * otherwise.
+ * Needs no workspace.  CQ_ERR_SHAPE for n_keep < 1 or > out_max_tokens, n_sinks + n_recent > n_keep, or an output that
+ * overlaps any other buffer, in part or whole, but in place.
  */
 int cq_evict(const float *mass, const void *k_codes, const void *v_codes, const int32_t *seq_lens, int n_seq, int n_heads,
              int head_dim, int c, int b, int64_t max_tokens, int64_t n_keep, int64_t n_sinks, int64_t n_recent,

@@ -49,6 +49,16 @@ int paged_shape(int64_t n_seq, int64_t n_rows, int max_q, int n_q_heads, int n_k
     return CQ_OK;
 }
 
+struct Extent {
+    const void* first;
+    size_t bytes;
+};
+bool overlap(const Extent& a, const Extent& b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.first), y = reinterpret_cast<uintptr_t>(b.first);
+    return x < y + b.bytes && y < x + a.bytes;
+}
+
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 int status(cudaError_t e) { return e == cudaSuccess ? CQ_OK : CQ_ERR_CUDA; }
 
@@ -291,6 +301,18 @@ int cq_evict(const float* mass, const void* k_codes, const void* v_codes, const 
     if (!aligned16(k_codes) || !aligned16(v_codes) || !aligned16(k_codes_out) || !aligned16(v_codes_out) || !aligned4(mass) || !aligned4(mass_out) ||
         !aligned4(seq_lens) || !aligned4(kept_out) || !aligned4(seq_lens_out))
         return CQ_ERR_ALIGN;
+    // what is written overlaps nothing else, apart from the buffers that are moved in place
+    const size_t rows = (size_t)n_seq * n_heads, out_blocks = (size_t)((out_max_tokens + kTokenBlock - 1) / kTokenBlock);
+    const size_t codes = rows * a.sh.n_blocks * a.sh.block_bytes, codes_out = rows * out_blocks * a.sh.block_bytes;
+    const Extent in[] = {{k_codes, codes}, {v_codes, codes}, {mass, rows * max_tokens * sizeof(float)}, {seq_lens, n_seq * sizeof(int32_t)}};
+    const Extent out[] = {{k_codes_out, codes_out}, {v_codes_out, codes_out}, {mass_out, rows * out_max_tokens * sizeof(float)},
+                          {kept_out, rows * n_keep * sizeof(int32_t)}, {seq_lens_out, n_seq * sizeof(int32_t)}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (overlap(out[i], in[j]) && !(same == 3 && i == j)) return CQ_ERR_SHAPE;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return CQ_ERR_SHAPE;
+    }
     a.mass = mass;
     a.kc = static_cast<const uint8_t*>(k_codes);
     a.vc = static_cast<const uint8_t*>(v_codes);

@@ -1029,7 +1029,7 @@ prefill_tc_kernel(const __half* __restrict__ q, const uint8_t* __restrict__ kc, 
         // ---- normalise and write: through shared memory (the codebooks are done with when the last sums are), so that the
         // stores take whole lines; a thread per row wrote 32 lines at a time (10.8 thousand cycles per CTA)
         if (n_tiles > 0) ok &= pf_wait(ctl, &ctl->pv_done[t], (uint32_t)(n_tiles - 1) & 1u);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, ok && !pf_failed(ctl));
         pf_fence_after();
         // no position: zero row; a wait gave up: NaN rows, so that nothing takes them for a result
         const float inv = !ok ? __int_as_float(0x7fffffff) : l > 0.f ? 1.f / l : 0.f;

@@ -441,8 +441,8 @@ int cq_decode_step_host(const void *q_host, const void *k_new_host, const void *
  *     t <= p   and   (window == 0  or  t < n_sinks  or  t > p - window),
  * so window counts the query's own token, and the n_sinks first tokens stay visible behind the window.  A query that sees
  * nothing (its position is negative, or no page is named for what it sees) gets a zero row.  A query with a NaN gets a row of
- * NaN, and so do the masses that it adds to; other rows are not touched by it.  Centroids have to be finite: a weight of zero
- * does not hide an infinite value.
+ * NaN, and so do the masses that it adds to; other rows are not touched by it.  (A score of minus infinity, which an infinite
+ * query can have, gives no weight.)  Centroids have to be finite: a weight of zero does not hide an infinite value.
  *
  * Kernels.  head_dim 128 with one byte per code, c = 2, 4 or 8: sequences with up to 16 (query token, query head of a KV head)
  * rows go through a kernel whose warps gather centroids from shared memory straight into tensor-core fragments, sequences
@@ -482,7 +482,7 @@ int cq_window_attn_variant(const void *q_fp16, const void *k_codes, const void *
  *   q_fp16, out_fp16   fp16 [n_rows][n_q_heads][head_dim]: the new tokens of all sequences, back to back
  *   q_offsets    [n_seq + 1] int32, device, ascending: the rows of sequence s are q_offsets[s] ... q_offsets[s + 1] - 1
  *                (none, one or many).  Rows of no sequence are left as they were in out.  Offsets are clamped to n_rows.
- *   max_q        no sequence has more new tokens (counts above are taken as max_q)
+ *   max_q        no sequence has more new tokens (counts above are taken as max_q); 1 ... pages_per_seq * page_tokens
  *   page_table   [n_seq][pages_per_seq] int32, device; entries that hold no attended token are not used, the tokens of an
  *                entry outside of [0, n_pages) count as absent
  *   seq_lens     [n_seq] int32, device: cached tokens, the new ones included
@@ -508,7 +508,7 @@ int cq_paged_attn_variant(const void *q_fp16, const int32_t *q_offsets, const vo
  * The way into the pages: the codes of the new tokens (cq_encode_kv's, with its fp32 codebooks) are written at the positions
  * seq_lens[s] - n ... seq_lens[s] - 1 of their sequences (q_offsets, page_table, seq_lens as in cq_paged_attn: the same
  * arrays serve both calls).  Positions outside of the capacity, and pages outside of the pool, are skipped; other positions
- * are untouched.  Two sequences must not have new tokens in the same page.
+ * are untouched.  Two sequences must not have new tokens in the same page, nor may a sequence name a page twice for them.
  *   k_fp16, v_fp16   fp16 [n_rows][n_heads][head_dim], 16-byte aligned;  k_pages, v_pages: two buffers
  */
 size_t cq_paged_append_workspace_bytes(int64_t n_rows, int n_heads, int head_dim, int c, int b);
@@ -526,8 +526,9 @@ int cq_paged_append(const void *k_fp16, const void *v_fp16, const int32_t *q_off
  *   mass_out     the same shape, may be mass_in; positions from seq_lens[s] on are left as they were
  *   workspace    cq_attn_mass_workspace_bytes(...) bytes, 16-byte aligned.  For up to four rows (query tokens x query heads of a
  *                KV head) they hold the scores between the two passes, 16 bytes per cached token and KV head.  What the same call
- *                with max_tokens = n_q_tokens asks for is enough for these: the second pass then works the scores out again.
- *                (Above 256 rows they hold the sums of every 256, 4 bytes per cached token and KV head.)
+ *                with max_tokens = n_q_tokens asks for is enough for these with variant 0: the second pass then works the scores
+ *                out again.  (Above floor(256 / R) query tokens, R being the query heads of a KV head, they hold the sums of
+ *                every floor(256 / R) of them, 4 bytes per cached token and KV head for each.)
  * Sums are formed in a fixed order: two calls on the same inputs give the same bits.
  * variant: as above (up to 16 rows of a sequence and KV head take the gather kernel, more the tcgen05 one).
  */

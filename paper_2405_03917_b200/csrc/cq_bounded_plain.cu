@@ -5,7 +5,10 @@
 //   codes_to_pages_kernel  codes of new tokens into the pages of their sequences
 //
 // One CTA per (row, query head), a token per warp and turn: the lanes hold the channels.  They stand in for the tuned kernels
-// at shapes that have none, and the tests compare both.
+// at shapes that have none, and the tests compare both.  What bounds them: a chain of dependent loads per token; one query each over
+// 16 x 4096 tokens, 32 heads on 8, takes 2.3 ms with CQ-8c10b and 1.3 ms with head_dim 64, masses 2.8 and 1.5 ms.
+// The way into the pages is the library's encode and one more launch: 64 x 1 tokens of 8 heads, CQ-8c8b, 9.0 us (5.8 of them the encode),
+// 4 x 2048 tokens 94 us (90).
 #include "cq_bounded.cuh"
 
 namespace cq {

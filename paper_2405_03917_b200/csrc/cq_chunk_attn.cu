@@ -3,16 +3,17 @@
 //
 // Attention.  What bounds it: per 64 tokens and 256 rows the MMAs take 1024 cycles of about 2160.  The rest is a chain: scores of a row tile
 // (tensor memory has room for one tile of them beside the outputs, queries and weights), their way into registers, the other row tile's
-// scores, at some 300 cycles for a hand-over: 4 x 2048 queries over 8192 tokens in pages of 64, 32 heads on 8, CQ-8c8b, 1.06 ms.  Two
-// threads share a row (3 x 333 queries with a window of 511, 32 heads of CQ-4c8b: 79 us with one, 55 with two; the prompts above are as fast
-// with one).  Half of the exponentials on the FMA pipe (1060 ... 1138 against 1046 us for those prompts), scores and weights in the same
+// scores, at some 300 cycles for a hand-over: 4 x 2048 queries over 8192 tokens, 32 heads on 8, CQ-8c8b, 1.07 ... 1.16 ms in pages of
+// 64, 0.99 ... 1.04 without (the plain prefill attention: 0.98 ... 1.03; side by side the look-up of pages costs 6 %).  Two
+// threads share a row (3 x 333 queries with a window of 511, 32 heads of CQ-4c8b: 79 us with one, 55 ... 61 with two; the prompts above are as
+// fast with one).  Half of the exponentials on the FMA pipe (1060 ... 1138 against 1046 us for those prompts), scores and weights in the same
 // columns (1186 against 978) and scores in halves (1152 against 988) were slower.  A context is shared by several CTAs where the row
 // tiles leave SMs idle.
 // Masses, from 17 rows of a sequence on.  A first pass leaves every row's log-sum-exp, a second one works the scores out again and adds up,
 // per token, the weights of a row tile: over the 32 rows of a warp by exchanges that halve the columns (lane i is left with column i), over the
 // warps through shared memory, over row tiles in a kernel of its own; every sum has one order.  What bounds it: the exponentials (two
 // passes, 16 per clock and SM) and the waits behind them: 1190 and 1660 cycles per 64 tokens of 128 rows.  A second tile of scores in the
-// outputs' columns changed nothing.  4 x 32 queries over 5001 ... 8192 tokens, 32 heads on 8, CQ-8c8b: 63 us, 227 us with the gather kernel.
+// outputs' columns changed nothing.  4 x 32 queries over 5001 ... 8192 tokens, 32 heads on 8, CQ-8c8b: 65 us, 227 us with the gather kernel.
 #include "cq_prefill_tc.cu"
 
 namespace cq {

@@ -9,14 +9,15 @@
 //       Masses crowd in few bins: every lane counts in a column of its own, so that the lanes of a warp never meet.  What bounds it is
 //       the number of instructions per token: 32 sequences x 40 heads of 8192 ... 32768 tokens: 345 us with a shared column per bin
 //       and all 32 bits by histograms, 280 us with columns of their own and masses read again for every pass, 161 us with masses in
-//       registers, room for the longest, 116 us with a loop for each of three lengths (105 MB of masses: 16 us).
+//       registers, room for the longest, 117 us with a loop for each of three lengths (105 MB of masses: 16 us).  Capacities above 32768
+//       do not fit the registers: 16 x 40 heads of 32768 tokens 208 us at that capacity, 317 us at 32784, move included.
 //   evict_move_kernel    a warp per 16 tokens that stay: a lane takes one (tensor, group) of them, a byte load per token (the
 //       lanes of a load read one token's codes: whole 16-token blocks pass through L1), and writes one 16-byte word.
-//       187 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
+//       186 us for the same call: it keeps 4096 of some 20000 tokens, and of ten 16-token blocks nine hold one that stays, so that
 //       nearly all codes are read (176 us with what is written, at the copy rate).
 //       (16-byte words of the source blocks instead, their bytes shifted in one by one: 268 us.)
 //       In place a CTA goes through its (sequence, head) in order: positions only ever move down, and all reads of a turn are done
-//       before its writes.
+//       before its writes: the same call takes 322 us in place, 303 into another cache (8 heads of 4097 tokens 29 and 11).
 #include "cq_bounded.cuh"
 
 namespace cq {

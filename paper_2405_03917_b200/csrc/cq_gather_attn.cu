@@ -18,8 +18,10 @@
 // travel by asynchronous copies.
 //
 // What bounds it: shared memory.  A token costs 4 wavefronts of centroids (of 5 in all) and 3 cycles of MMAs; a block of 16 tokens
-// takes about 115 cycles, 80 of them wavefronts.  64 sequences, 32 heads on 8, CQ-8c8b: window of 4096 81 us, contexts of
-// 4096 ... 16384 in pages 166 us = 1.0 TB/s.
+// takes about 110 cycles, 82 of them wavefronts.  64 sequences, 32 heads on 8, CQ-8c8b: window of 4096 82 us, contexts of
+// 4096 ... 16384 in pages 165 us = 1.0 TB/s; of 16384 without a window 239 us, as long as the table kernels of the plain decode
+// attention take (238; 64 heads on 8 by eight rows: 256 and 433).  With a KV head to every query head a whole centroid is gathered where
+// those read one table entry: 16 x 4096, 32 heads of CQ-4c8b 91 us (60 there), 40 heads of CQ-8c8b 96 us (52).
 //
 // Masses take two passes: kLse leaves every row's log-sum-exp and, for up to four rows, the scores; mass_of_scores_kernel turns these into
 // weights and adds up, per token, those of all rows.  Where scores are not kept, kMass works them out again.  (Row after row tile goes

@@ -70,6 +70,14 @@ def test_conversations_next_to_a_chunk(recorder):
     assert check(recorder, SERVED) > 0
 
 
+@pytest.mark.parametrize("R,n_q", [(1, 256), (1, 257), (3, 85), (3, 86), (4, 200), (100, 2), (100, 3), (100, 9)])
+def test_masses_of_several_row_tiles_hold_their_sums(R, n_q):
+    # floor(256 / R) query tokens to a row tile; above one, 4 bytes per cached token and KV head for each
+    n_seq, hkv, tiles = 64, 4, -(-n_q // (256 // R))
+    size = lambda cap: cq.cq_attn_mass_workspace_bytes(n_seq, n_q, R * hkv, hkv, 128, 8, 8, cap)
+    assert size(4096) - size(2048) == (4 * n_seq * hkv * 2048 * tiles if tiles > 1 else 0)
+
+
 def test_random_mixes(recorder):
     rng = random.Random(7)
     mixes = []
